@@ -70,6 +70,8 @@ extern "C" {
                                          beyond it may have no output */
 #define WUSHKV_DEV_VALUE_RANGE    32  /* a stored value step Delta_v >= 1024: beyond the fp16 range of the decode value contraction */
 #define WUSHKV_DEV_ROPE_RANGE     64  /* a position beyond the rotary table of a *_projected call: rotated by the table's last angle */
+#define WUSHKV_DEV_POOL_EMPTY    128  /* wushkv_pages_reserve: too few free pages, none was handed out */
+#define WUSHKV_DEV_BAD_REFS      256  /* a page's reference count contradicts the page table */
 /* After PAGE_TABLE_FULL, BAD_PAGE_ID, BAD_SLOT or BAD_COUNT in wushkv_append the length of the affected
  * sequence is left as it was (tokens of the call that did fit are orphaned: nothing reads them). */
 
@@ -368,6 +370,115 @@ int wushkv_decode_step_host(const wushkv_cache* cache, int32_t batch, const int3
                             const uint16_t* K_new_host, const uint16_t* V_new_host, const uint16_t* Q_host,
                             float* O_host, void* staging, size_t staging_bytes,
                             void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Sparse decode attention: the new query of a sequence attends to the windows (first S_sink and recent positions, always) and
+ * to at most n_select of the packed pages, those whose keys promise the largest scores, instead of to all.  (The paper attends
+ * to every position; the selection is an option for long caches.)
+ *
+ * Page bounds.  Beside a packed page, per KV head:
+ *   bounds (device): int8 [n_pages][n_kv][2][d], [0] lower and [1] upper bound of every channel, 16-byte aligned;
+ *   exponents (device): int8 [n_pages][n_kv].
+ * Over the tokens of the page that exist, with khat = x_min + Delta code rounded to fp32:
+ *   e = least integer >= -31 with max |khat| <= 127 * 2^e,  lower = floor(min khat / 2^e),  upper = ceil(max khat / 2^e).
+ * wushkv_update_page_bounds computes them for all pages that hold one of the positions [seq_len[b] - n_new[b], seq_len[b]),
+ * n_new[b] = cu_new[b+1] - cu_new[b]: call it after wushkv_append with the same slot, cu_new and max_new (a larger max_new is
+ * fine, a smaller one leaves pages out), seq_len being the lengths after that append.  The pages of other positions are left as
+ * they are.  Pages that the append refused are skipped and flagged.  batch <= 65535.
+ *
+ * Selection.  wushkv_select_pages lists, per sequence and KV head, min(n_select, packed pages) page indexes (of the page table's
+ * row) in ascending order, -1 in the places behind:
+ *   selected (device, out): int32 [batch][n_kv][n_select].
+ * q' = T_K^{-T} q (double precision) is rounded to qi = round(q' * 32512 / max|q'|).  The score of a page for a query head is
+ *   s = 2^e * sum_c (max(qi_c, 0) upper_c + min(qi_c, 0) lower_c) * (max|q'| / 32512 * sm_scale),
+ * an upper bound of the logits of all its tokens (for the rounded query); the sum is an exact integer, s is rounded to fp32
+ * after the conversion of the sum and after the product.  A page's key is max over the query heads of the group of
+ * (s - largest s of all pages of that head): how far the page is, for the head it matters most to, below that head's best page.
+ * The n_select pages with the largest keys are taken, of equal keys the lower index.  The result depends on the inputs alone.
+ * A query that is zero or not finite scores 0 everywhere.  Sequences may have up to 1 048 576 cached positions
+ * (WUSHKV_ECAPACITY for a larger max_seq_len); one that exceeds max_seq_len is flagged with BAD_COUNT and its pages beyond are not
+ * candidates.
+ *
+ * Attention.  wushkv_decode_attn_selected attends to the windows and the listed pages:
+ *   selected (device): int32 [batch][n_kv][n_select]; of a row the first min(n_select, packed pages) entries are read; they must
+ *   be distinct; -1 is skipped, an index outside the sequence's packed pages is skipped and flagged with BAD_PAGE_ID.  Positions
+ *   of a listed page that a window holds are read from the window, as always.  Lists need not come from wushkv_select_pages.
+ *   O (device, out): bf16 [batch][n_q][d], 16-byte aligned (the rounding is smaller than what a selection leaves out).
+ * wushkv_decode_attn_sparse is both in one call, the selection running beside the preparation of the queries.
+ * prologue: NULL, or the Norm / RoPE of projected queries (as in wushkv_decode_attn_projected).
+ * The other arguments are those of wushkv_decode_attn; workspace: >= wushkv_sparse_workspace_bytes() bytes, 256-byte aligned,
+ * scratch.  A sequence may be named by several rows of a call with different lengths (tokens to verify), as long as the ring
+ * still holds the recent window of the shortest.
+ */
+int wushkv_update_page_bounds(const wushkv_cache* cache, int32_t batch, const int32_t* slot, const int32_t* seq_len,
+                              const int32_t* cu_new, int32_t max_new, int8_t* bounds, int8_t* exponents, void* stream);
+int wushkv_select_pages(const wushkv_cache* cache, int32_t batch, const int32_t* slot, const int32_t* seq_len, int32_t max_seq_len,
+                        const uint16_t* Q, const wushkv_prologue* prologue, const int8_t* bounds, const int8_t* exponents,
+                        int32_t n_select, int32_t* selected, void* stream);
+size_t wushkv_sparse_workspace_bytes(const wushkv_cache* cache, int32_t batch, int32_t max_seq_len, int32_t n_select);
+int wushkv_decode_attn_selected(const wushkv_cache* cache, int32_t batch, const int32_t* slot, const int32_t* seq_len, int32_t max_seq_len,
+                                const uint16_t* Q, const wushkv_prologue* prologue, const int32_t* selected, int32_t n_select,
+                                uint16_t* O, void* workspace, size_t workspace_bytes, void* stream);
+int wushkv_decode_attn_sparse(const wushkv_cache* cache, int32_t batch, const int32_t* slot, const int32_t* seq_len, int32_t max_seq_len,
+                              const uint16_t* Q, const wushkv_prologue* prologue, const int8_t* bounds, const int8_t* exponents,
+                              int32_t n_select, int32_t* selected, uint16_t* O, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Management of the pages: which page of the pool holds which part of which sequence.  (The paper fixes nothing here.)  The
+ * bookkeeping of a pool can serve all layers that share a page table: the calls on a wushkv_page_pool run once per step, the
+ * copies that follow from them (wushkv_copy_pages, wushkv_copy_windows) once per layer.  Everything stays on the device and
+ * may be captured into a graph.
+ *   page_table (device, in/out): int32 [n_slots][max_pages], the table that the layers' wushkv_cache names.  -1: no page.
+ *     An entry <= -2 is a locked page, -2 - page (see wushkv_pages_reserve); appends and attention refuse it like any id outside
+ *     the pool (BAD_PAGE_ID).
+ *   refs (device, in/out): int32 [n_pages], number of table entries that name the page; 0: the page is free.
+ *   dev_status (device): error bits, as in wushkv_cache.
+ * The caller starts with a table of -1 and counts of 0 (or with counts that match its table).
+ *
+ * wushkv_pages_reserve: before wushkv_append of the tokens (seq_len, cu_new as the append will get them), gives every sequence
+ *   the pages that its new tokens will be written to.  Indexes without a page get a free one.  If the last page is partly filled
+ *   and other entries name it too, the sequence gets a page of its own and the old one is to be copied into it: the pair is
+ *   appended to the copy list, which the caller passes to wushkv_copy_pages before the append.  Sequences are taken in order,
+ *   pages within a sequence too, free pages lowest first; if all holders of a page reserve in one call, the last keeps it.
+ *     copy_src, copy_dst (device, out): int32 [batch], pairs of page ids, -1 behind them; n_copies (device, out): their number.
+ *   If there are fewer free pages than the call needs, none is handed out: WUSHKV_DEV_POOL_EMPTY is set, missing pages stay
+ *   missing, and the entry of a partly filled page that others name is locked, so that an append of that sequence is refused
+ *   (BAD_PAGE_ID, length unchanged) and cannot write into the others' page.  A later call that succeeds unlocks it.  A sequence
+ *   whose tokens pass the table's end gets nothing (PAGE_TABLE_FULL).  Slots must be distinct (not checked).
+ *   workspace (device): >= wushkv_pages_workspace_bytes(pool, batch) bytes, 4-byte aligned, scratch.
+ * wushkv_pages_fork: for k < n, sequence dst_slot[k] becomes a copy of sequence src_slot[k] of src_len[k] cached positions (its
+ *   current length): their pages are shared.  What dst_slot[k] held before is given back.  A destination must not be another
+ *   destination or a source of the same call (not checked; counts stay consistent).  Follow with wushkv_copy_windows per layer.
+ * wushkv_pages_release: gives back the pages of slot[k] beyond its first keep_len[k] positions (keep_len NULL: all).  A sequence
+ *   that goes on from a shorter length needs its recent window in the ring: the ring holds the last ring_cap positions written.
+ *   The same slot may be named twice.
+ * wushkv_pages_compact: moves the live pages to the ids 0 .. live - 1: the k-th live page with an id >= live (ascending) goes to
+ *   the k-th free id below.  Table and counts are rewritten, locked entries stay locked.
+ *     copy_src, copy_dst (device, out): int32 [(n_pages + 1) / 2], pairs for wushkv_copy_pages, -1 behind them;
+ *     n_copies, n_live (device, out): int32 each.  workspace as above (any batch).
+ *   The copies must be done (every layer) before the next call that reads or writes pages.
+ * wushkv_copy_pages: copies whole pages of one layer, pair by pair, with their bounds and exponents unless those are NULL.
+ *   max_copies (host): capacity of the list; n_copies (device): its length.  No destination may be a source of the list.
+ * wushkv_copy_windows: copies the bf16 sink and ring rows that src_len[k] positions of src_slot[k] use (one layer) to
+ *   dst_slot[k]; other rows are left as they were.  Destinations must not be sources.  n <= 65535.
+ */
+typedef struct wushkv_page_pool {
+    int32_t n_slots, max_pages;
+    int64_t n_pages;
+    int32_t* page_table;
+    int32_t* refs;
+    int32_t* dev_status;
+} wushkv_page_pool;
+size_t wushkv_pages_workspace_bytes(const wushkv_page_pool* pool, int32_t batch);
+int wushkv_pages_reserve(const wushkv_page_pool* pool, int32_t batch, const int32_t* slot, const int32_t* seq_len, const int32_t* cu_new,
+                         int32_t* copy_src, int32_t* copy_dst, int32_t* n_copies, void* workspace, size_t workspace_bytes, void* stream);
+int wushkv_pages_fork(const wushkv_page_pool* pool, int32_t n, const int32_t* src_slot, const int32_t* dst_slot, const int32_t* src_len, void* stream);
+int wushkv_pages_release(const wushkv_page_pool* pool, int32_t n, const int32_t* slot, const int32_t* keep_len, void* stream);
+int wushkv_pages_compact(const wushkv_page_pool* pool, int32_t* copy_src, int32_t* copy_dst, int32_t* n_copies, int32_t* n_live,
+                         void* workspace, size_t workspace_bytes, void* stream);
+int wushkv_copy_pages(const wushkv_cache* cache, int32_t max_copies, const int32_t* copy_src, const int32_t* copy_dst, const int32_t* n_copies,
+                      int8_t* bounds, int8_t* exponents, void* stream);
+int wushkv_copy_windows(const wushkv_cache* cache, int32_t n, const int32_t* src_slot, const int32_t* dst_slot, const int32_t* src_len, void* stream);
 
 /*
  * wushkv_decode_attn without a caller-provided workspace (the paper has no counterpart: this is

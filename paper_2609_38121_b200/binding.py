@@ -15,7 +15,7 @@ LIB_PATH = os.path.join(_HERE, "libwushkv.so")
 OK, EINVAL, ENOTPD, ECUDA, ECAPACITY = 0, 1, 2, 3, 4
 QUANTIZER_AFFINE, QUANTIZER_QUEST = 0, 1
 DEV_PAGE_TABLE_FULL, DEV_BAD_PAGE_ID, DEV_BAD_SLOT, DEV_COPY_TIMEOUT, DEV_BAD_COUNT, DEV_VALUE_RANGE = 1, 2, 4, 8, 16, 32
-DEV_ROPE_RANGE = 64
+DEV_ROPE_RANGE, DEV_POOL_EMPTY, DEV_BAD_REFS = 64, 128, 256
 
 EXPORTS = (
     "wushkv_page_bytes", "wushkv_status_string", "wushkv_accumulate_gram", "wushkv_build_transforms",
@@ -26,6 +26,9 @@ EXPORTS = (
     "wushkv_build_rope_table", "wushkv_append_projected", "wushkv_decode_attn_projected",
     "wushkv_attention_hessians_workspace_bytes", "wushkv_accumulate_attention_hessians_device",
     "wushkv_prefill_attn_projected",
+    "wushkv_update_page_bounds", "wushkv_select_pages", "wushkv_sparse_workspace_bytes", "wushkv_decode_attn_selected",
+    "wushkv_decode_attn_sparse", "wushkv_pages_workspace_bytes", "wushkv_pages_reserve", "wushkv_pages_fork",
+    "wushkv_pages_release", "wushkv_pages_compact", "wushkv_copy_pages", "wushkv_copy_windows",
 )
 STATIC_SCRATCH_BYTES = 8 << 20
 
@@ -55,6 +58,12 @@ class wushkv_prologue(C.Structure):
     """Mirror of ``struct wushkv_prologue`` (device pointers)."""
     _fields_ = [("rope_table", C.c_void_p), ("rope_positions", C.c_int32), ("normalise", C.c_int32),
                 ("k_norm_weight", C.c_void_p), ("q_norm_weight", C.c_void_p), ("norm_eps", C.c_float)]
+
+
+class wushkv_page_pool(C.Structure):
+    """Mirror of ``struct wushkv_page_pool`` (device pointers)."""
+    _fields_ = [("n_slots", C.c_int32), ("max_pages", C.c_int32), ("n_pages", C.c_int64),
+                ("page_table", C.c_void_p), ("refs", C.c_void_p), ("dev_status", C.c_void_p)]
 
 
 def _load():
@@ -129,6 +138,21 @@ def _load():
     lib.wushkv_accumulate_attention_hessians_device.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_void_p,
                                                                 C.c_void_p, C.c_void_p, C.c_void_p, C.c_double, C.c_void_p,
                                                                 C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    cache, pool, prologue, i32, ptr, size = C.POINTER(wushkv_cache), C.POINTER(wushkv_page_pool), C.POINTER(wushkv_prologue), C.c_int32, C.c_void_p, C.c_size_t
+    for name, result, args in (
+            ("wushkv_update_page_bounds", C.c_int, [cache, i32, ptr, ptr, ptr, i32, ptr, ptr, ptr]),
+            ("wushkv_select_pages", C.c_int, [cache, i32, ptr, ptr, i32, ptr, prologue, ptr, ptr, i32, ptr, ptr]),
+            ("wushkv_sparse_workspace_bytes", size, [cache, i32, i32, i32]),
+            ("wushkv_decode_attn_selected", C.c_int, [cache, i32, ptr, ptr, i32, ptr, prologue, ptr, i32, ptr, ptr, size, ptr]),
+            ("wushkv_decode_attn_sparse", C.c_int, [cache, i32, ptr, ptr, i32, ptr, prologue, ptr, ptr, i32, ptr, ptr, ptr, size, ptr]),
+            ("wushkv_pages_workspace_bytes", size, [pool, i32]),
+            ("wushkv_pages_reserve", C.c_int, [pool, i32, ptr, ptr, ptr, ptr, ptr, ptr, ptr, size, ptr]),
+            ("wushkv_pages_fork", C.c_int, [pool, i32, ptr, ptr, ptr, ptr]),
+            ("wushkv_pages_release", C.c_int, [pool, i32, ptr, ptr, ptr]),
+            ("wushkv_pages_compact", C.c_int, [pool, ptr, ptr, ptr, ptr, ptr, size, ptr]),
+            ("wushkv_copy_pages", C.c_int, [cache, i32, ptr, ptr, ptr, ptr, ptr, ptr]),
+            ("wushkv_copy_windows", C.c_int, [cache, i32, ptr, ptr, ptr, ptr])):
+        getattr(lib, name).restype, getattr(lib, name).argtypes = result, args
     lib.wushkv_set_test_option.restype = C.c_int
     lib.wushkv_set_test_option.argtypes = [C.c_char_p, C.c_longlong]
     return lib
@@ -352,6 +376,83 @@ def prefill_attn(cache: wushkv_cache, batch, slot, seq_len, cu_new, total_new, m
                                    _stream_ptr(stream)), "wushkv_prefill_attn")
 
 
+def update_page_bounds(cache: wushkv_cache, batch, slot, seq_len, cu_new, max_new, bounds, exponents, stream=None):
+    """wushkv_update_page_bounds: bounds int8 [n_pages][n_kv][2][d] and exponents int8 [n_pages][n_kv] of the pages that hold the
+    last cu_new[b+1] - cu_new[b] of seq_len[b] positions (device tensors; after the append)."""
+    _check(lib.wushkv_update_page_bounds(C.byref(cache), batch, _ptr(slot), _ptr(seq_len), _ptr(cu_new), max_new, _ptr(bounds),
+                                         _ptr(exponents), _stream_ptr(stream)), "wushkv_update_page_bounds")
+
+
+def _prologue_ptr(prologue):
+    return None if prologue is None else C.byref(prologue)
+
+
+def select_pages(cache: wushkv_cache, batch, slot, seq_len, max_seq_len, Q, bounds, exponents, n_select, selected, prologue=None,
+                 stream=None):
+    """wushkv_select_pages: selected int32 [batch][n_kv][n_select], page indexes in ascending order, -1 behind them."""
+    _check(lib.wushkv_select_pages(C.byref(cache), batch, _ptr(slot), _ptr(seq_len), max_seq_len, _ptr(Q), _prologue_ptr(prologue),
+                                   _ptr(bounds), _ptr(exponents), n_select, _ptr(selected), _stream_ptr(stream)), "wushkv_select_pages")
+
+
+def sparse_workspace_bytes(cache: wushkv_cache, batch: int, max_seq_len: int, n_select: int) -> int:
+    return int(lib.wushkv_sparse_workspace_bytes(C.byref(cache), batch, max_seq_len, n_select))
+
+
+def decode_attn_selected(cache: wushkv_cache, batch, slot, seq_len, max_seq_len, Q, selected, n_select, O, workspace, workspace_bytes,
+                         prologue=None, stream=None):
+    """wushkv_decode_attn_selected: attention over the windows and the listed pages; O bf16 [batch][n_q][d]."""
+    _check(lib.wushkv_decode_attn_selected(C.byref(cache), batch, _ptr(slot), _ptr(seq_len), max_seq_len, _ptr(Q),
+                                           _prologue_ptr(prologue), _ptr(selected), n_select, _ptr(O), _ptr(workspace), workspace_bytes,
+                                           _stream_ptr(stream)), "wushkv_decode_attn_selected")
+
+
+def decode_attn_sparse(cache: wushkv_cache, batch, slot, seq_len, max_seq_len, Q, bounds, exponents, n_select, selected, O, workspace,
+                       workspace_bytes, prologue=None, stream=None):
+    """wushkv_decode_attn_sparse: select_pages (into ``selected``) and decode_attn_selected in one call."""
+    _check(lib.wushkv_decode_attn_sparse(C.byref(cache), batch, _ptr(slot), _ptr(seq_len), max_seq_len, _ptr(Q), _prologue_ptr(prologue),
+                                         _ptr(bounds), _ptr(exponents), n_select, _ptr(selected), _ptr(O), _ptr(workspace),
+                                         workspace_bytes, _stream_ptr(stream)), "wushkv_decode_attn_sparse")
+
+
+def pages_workspace_bytes(pool: wushkv_page_pool, batch: int) -> int:
+    return int(lib.wushkv_pages_workspace_bytes(C.byref(pool), batch))
+
+
+def pages_reserve(pool: wushkv_page_pool, batch, slot, seq_len, cu_new, copy_src, copy_dst, n_copies, workspace, workspace_bytes,
+                  stream=None):
+    """wushkv_pages_reserve: pages for the tokens that the next append brings; copy_src / copy_dst int32 [batch], n_copies int32 [1]."""
+    _check(lib.wushkv_pages_reserve(C.byref(pool), batch, _ptr(slot), _ptr(seq_len), _ptr(cu_new), _ptr(copy_src), _ptr(copy_dst),
+                                    _ptr(n_copies), _ptr(workspace), workspace_bytes, _stream_ptr(stream)), "wushkv_pages_reserve")
+
+
+def pages_fork(pool: wushkv_page_pool, n, src_slot, dst_slot, src_len, stream=None):
+    """wushkv_pages_fork: the sequences in dst_slot become copies of those in src_slot and share their pages."""
+    _check(lib.wushkv_pages_fork(C.byref(pool), n, _ptr(src_slot), _ptr(dst_slot), _ptr(src_len), _stream_ptr(stream)), "wushkv_pages_fork")
+
+
+def pages_release(pool: wushkv_page_pool, n, slot, keep_len=None, stream=None):
+    """wushkv_pages_release: gives back the pages of the slots beyond their first keep_len positions (None: all)."""
+    _check(lib.wushkv_pages_release(C.byref(pool), n, _ptr(slot), _ptr(keep_len), _stream_ptr(stream)), "wushkv_pages_release")
+
+
+def pages_compact(pool: wushkv_page_pool, copy_src, copy_dst, n_copies, n_live, workspace, workspace_bytes, stream=None):
+    """wushkv_pages_compact: live pages to the lowest ids; copy_src / copy_dst int32 [(n_pages + 1) // 2] for copy_pages."""
+    _check(lib.wushkv_pages_compact(C.byref(pool), _ptr(copy_src), _ptr(copy_dst), _ptr(n_copies), _ptr(n_live), _ptr(workspace),
+                                    workspace_bytes, _stream_ptr(stream)), "wushkv_pages_compact")
+
+
+def copy_pages(cache: wushkv_cache, max_copies, copy_src, copy_dst, n_copies, bounds=None, exponents=None, stream=None):
+    """wushkv_copy_pages: copies one layer's pages (and their bounds) by a list that pages_reserve or pages_compact wrote."""
+    _check(lib.wushkv_copy_pages(C.byref(cache), max_copies, _ptr(copy_src), _ptr(copy_dst), _ptr(n_copies), _ptr(bounds),
+                                 _ptr(exponents), _stream_ptr(stream)), "wushkv_copy_pages")
+
+
+def copy_windows(cache: wushkv_cache, n, src_slot, dst_slot, src_len, stream=None):
+    """wushkv_copy_windows: copies one layer's bf16 window rows of the sequences in src_slot to dst_slot."""
+    _check(lib.wushkv_copy_windows(C.byref(cache), n, _ptr(src_slot), _ptr(dst_slot), _ptr(src_len), _stream_ptr(stream)),
+           "wushkv_copy_windows")
+
+
 def set_test_option(name: str, value: int):
     """wushkv_set_test_option: process-wide testing aids (see the header for the names)."""
     _check(lib.wushkv_set_test_option(name.encode(), int(value)), "wushkv_set_test_option")
@@ -359,21 +460,34 @@ def set_test_option(name: str, value: int):
 
 class PagedCache:
     """Owns the device buffers of one layer's cache (torch tensors) and the filled ``wushkv_cache``
-    descriptor.  Pure bookkeeping: page-table assignment and allocation, no arithmetic."""
+    descriptor.  Pure bookkeeping: page-table assignment and allocation, no arithmetic.
+
+    Every slot owns the pages of max_seq_len positions from the start, unless ``pool`` is given: then pages come from that
+    PagePool as sequences need them.  ``page_bounds``: allocates the bounds that sparse attention selects pages by."""
 
     def __init__(self, n_q, n_kv, bits, n_slots, max_seq_len, s_sink, s_keep, s_flush, kappa_k, kappa_v,
-                 T_K, T_K_invT, sm_scale=None, boundary_lag=0, ring_cap=None, device="cuda", page_order=None, quantizer=0):
+                 T_K, T_K_invT, sm_scale=None, boundary_lag=0, ring_cap=None, device="cuda", page_order=None, quantizer=0,
+                 pool=None, page_bounds=False):
         import torch
         d, page_tokens = 128, 64
         self.torch = torch
         self.device = torch.device(device)
         self.n_q, self.n_kv, self.bits, self.n_slots = n_q, n_kv, bits, n_slots
         self.max_pages = (max_seq_len + page_tokens - 1) // page_tokens
-        n_pages = n_slots * self.max_pages
+        if pool is not None and (pool.n_slots, pool.max_pages) != (n_slots, self.max_pages):
+            raise ValueError("the pool's page table has other slots or lengths than this cache")
+        n_pages = n_slots * self.max_pages if pool is None else pool.n_pages
         self.page_bytes = page_bytes(n_kv, d, bits, page_tokens)
         self.pages = torch.zeros(n_pages * self.page_bytes, dtype=torch.uint8, device=self.device)
-        order = np.arange(n_pages) if page_order is None else np.asarray(page_order)
-        self.page_table = torch.from_numpy(order.reshape(n_slots, self.max_pages).astype(np.int32)).to(self.device)
+        if pool is None:
+            order = np.arange(n_pages) if page_order is None else np.asarray(page_order)
+            self.page_table = torch.from_numpy(order.reshape(n_slots, self.max_pages).astype(np.int32)).to(self.device)
+        else:
+            self.page_table = pool.page_table
+        self.bounds = self.exponents = None
+        if page_bounds:
+            self.bounds = torch.zeros((n_pages, n_kv, 2, d), dtype=torch.int8, device=self.device)
+            self.exponents = torch.zeros((n_pages, n_kv), dtype=torch.int8, device=self.device)
         self.ring_cap = ring_cap if ring_cap is not None else s_keep + s_flush - 1 + boundary_lag
         self.sink_kv = torch.zeros((n_slots, n_kv, 2, max(s_sink, 1), d), dtype=torch.bfloat16, device=self.device)
         self.ring_kv = torch.zeros((n_slots, n_kv, 2, self.ring_cap, d), dtype=torch.bfloat16, device=self.device)
@@ -387,6 +501,55 @@ class PagedCache:
             quantizer=quantizer, n_pages=n_pages, pages=self.pages.data_ptr(), page_table=self.page_table.data_ptr(),
             sink_kv=self.sink_kv.data_ptr(), ring_kv=self.ring_kv.data_ptr(), T_K=self.T_K.data_ptr(),
             T_K_invT=self.T_K_invT.data_ptr(), dev_status=self.dev_status.data_ptr())
+
+    def status(self) -> int:
+        return int(self.dev_status.item())
+
+
+class PagePool:
+    """The page table and the reference counts of a pool of pages, for all layers (PagedCache with ``pool``) that share them.
+    The methods act on the table and then copy, for each of the caches given, what has to be copied; nothing synchronises."""
+
+    def __init__(self, n_slots, max_seq_len, n_pages, max_batch=None, device="cuda"):
+        import torch
+        self.torch, self.device = torch, torch.device(device)
+        self.n_slots, self.max_pages, self.n_pages = n_slots, (max_seq_len + 63) // 64, n_pages
+        ints = lambda *shape, value=0: torch.full(shape, value, dtype=torch.int32, device=self.device)  # noqa: E731
+        self.page_table, self.refs = ints(n_slots, self.max_pages, value=-1), ints(n_pages)
+        self.dev_status, self.n_copies, self.n_live = ints(1), ints(1), ints(1)
+        self.max_batch = n_slots if max_batch is None else max_batch
+        self.copies = ints(2, max(self.max_batch, (n_pages + 1) // 2), value=-1)
+        self.desc = wushkv_page_pool(n_slots=n_slots, max_pages=self.max_pages, n_pages=n_pages, page_table=_ptr(self.page_table),
+                                     refs=_ptr(self.refs), dev_status=_ptr(self.dev_status))
+        self.workspace_bytes = pages_workspace_bytes(self.desc, self.max_batch)
+        self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
+
+    def _copy(self, caches, capacity, stream):
+        for cache in caches:
+            copy_pages(cache.desc, capacity, self.copies[0], self.copies[1], self.n_copies, cache.bounds, cache.exponents, stream)
+
+    def reserve(self, caches, batch, slot, seq_len, cu_new, stream=None):
+        """Pages for the tokens that the next append brings; shared last pages are copied first."""
+        if batch > self.max_batch:
+            raise ValueError("more sequences than the pool's max_batch")
+        pages_reserve(self.desc, batch, slot, seq_len, cu_new, self.copies[0], self.copies[1], self.n_copies, self.workspace,
+                      self.workspace_bytes, stream)
+        self._copy(caches, batch, stream)
+
+    def fork(self, caches, n, src_slot, dst_slot, src_len, stream=None):
+        """The sequences in dst_slot become copies of those in src_slot (src_len positions each)."""
+        pages_fork(self.desc, n, src_slot, dst_slot, src_len, stream)
+        for cache in caches:
+            copy_windows(cache.desc, n, src_slot, dst_slot, src_len, stream)
+
+    def release(self, n, slot, keep_len=None, stream=None):
+        """Gives back the pages of the slots beyond their first keep_len positions (None: all)."""
+        pages_release(self.desc, n, slot, keep_len, stream)
+
+    def compact(self, caches, stream=None):
+        """Moves the live pages of all caches to the lowest ids; their number is left in ``n_live``."""
+        pages_compact(self.desc, self.copies[0], self.copies[1], self.n_copies, self.n_live, self.workspace, self.workspace_bytes, stream)
+        self._copy(caches, (self.n_pages + 1) // 2, stream)
 
     def status(self) -> int:
         return int(self.dev_status.item())

@@ -40,6 +40,7 @@
 #include "host_common.h"
 #include "prologue.cuh"
 #include "layout.cuh"
+#include "sparse.cuh"
 
 namespace wushkv {
 
@@ -82,6 +83,9 @@ struct DecodeParams {
     int q_early;         // 1: Q was final before the kernel ahead of the preparation kernel started
     int stream_pages;    // 1: the packed pages of a step cannot stay in L2 anyway: copy them with an evict-first hint
     Prologue pro;        // pro.rope != nullptr: Q holds projected queries, normalised and rotated by the preparation kernel
+    const int* selected; // [batch][n_kv][n_select]: sparse attention, the packed pages that a (sequence, KV head) reads (-1: none)
+    int n_select;        // 0: dense attention
+    unsigned short* O16; // sparse attention: the outputs as bf16 (O is not used)
 };
 
 // Arrival counters of a (sequence, KV head)'s 8 query head slots for the main kernel's merge, zeroed by the preparation kernel:
@@ -124,6 +128,12 @@ __device__ __forceinline__ SeqInfo seq_info(const CacheView& c, int S, int slot)
     si.recent_lo = c.s_sink + nq;
     si.n_win = si.n_sink + max(0, S - si.recent_lo);
     si.U = si.qp + (si.n_win + WIN_TOKENS - 1) / WIN_TOKENS;
+    return si;
+}
+
+// Sparse attention reads at most n_select of the packed pages, the first min(n_select, qp) entries of the (sequence, KV head)'s list.
+__device__ __forceinline__ SeqInfo sparse_info(SeqInfo si, int n_select) {
+    if (si.qp > n_select) { si.U -= si.qp - n_select; si.qp = n_select; }
     return si;
 }
 
@@ -208,7 +218,10 @@ __global__ void __launch_bounds__(PREP_THREADS) decode_prep_kernel(DecodeParams 
         for (int base = 0; base < P.batch; base += 128) {
             const int bb = base + i;
             long long u = 0;
-            if (i < 128 && bb < P.batch) u = seq_info(P.c, __ldcg(P.seq_len + bb), __ldg(P.slot + bb)).U;
+            if (i < 128 && bb < P.batch) {
+                const SeqInfo si = seq_info(P.c, __ldcg(P.seq_len + bb), __ldg(P.slot + bb));
+                u = P.n_select > 0 ? sparse_info(si, P.n_select).U : si.U;
+            }
             long long incl = u;
             for (int o = 1; o < 32; o <<= 1) {
                 const long long v = __shfl_up_sync(FULL, incl, o);
@@ -490,10 +503,14 @@ struct WarpState {
     }
 };
 
+// An output, as fp32 or (sparse attention) rounded to bf16: what a selection of pages leaves out is larger than that rounding.
+__device__ __forceinline__ void put_output(float* p, float x) { *p = x; }
+__device__ __forceinline__ void put_output(unsigned short* p, float x) { *p = __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
+
 // Writes this warp's state of every query head of one (sequence, KV head) to global memory: a partial (max, sum, o[128]) in
-// records PART_STRIDE floats apart, or, WHOLE, the head's outputs o / sum in rows of D floats.
-template <int BITS, int MODE, bool WHOLE>
-__device__ __forceinline__ void store_state(const WarpState<MODE>& st, float* dst0, int lane, int G) {
+// records PART_STRIDE floats apart, or, WHOLE, the head's outputs o / sum in rows of D numbers.
+template <int BITS, int MODE, bool WHOLE, class Out>
+__device__ __forceinline__ void store_state(const WarpState<MODE>& st, Out* dst0, int lane, int G) {
     const int g = lane >> 2, t = lane & 3;
     constexpr int NH = WarpState<MODE>::NH;
 #pragma unroll
@@ -504,7 +521,7 @@ __device__ __forceinline__ void store_state(const WarpState<MODE>& st, float* ds
         l += __shfl_xor_sync(FULL, l, 16); z += __shfl_xor_sync(FULL, z, 16);
         const int head = MODE == 0 ? t : 2 * t + k;
         if (head < G) {
-            float* dst = dst0 + head * (WHOLE ? D : PART_STRIDE);
+            Out* dst = dst0 + head * (WHOLE ? D : PART_STRIDE);
             if (!WHOLE) {
                 if (g == 0) { dst[0] = st.m[k]; dst[1] = l; }
                 dst += 4;
@@ -524,8 +541,8 @@ __device__ __forceinline__ void store_state(const WarpState<MODE>& st, float* ds
                     lo_ch = l > 0.f ? lo_ch / l : 0.f;
                     hi_ch = l > 0.f ? hi_ch / l : 0.f;
                 }
-                dst[16 * i + g] = lo_ch;
-                dst[16 * i + g + 8] = hi_ch;
+                put_output(dst + 16 * i + g, lo_ch);
+                put_output(dst + 16 * i + g + 8, hi_ch);
             }
         }
     }
@@ -652,6 +669,10 @@ struct MergedState {
         const bool any = l > 0.f;
         reinterpret_cast<float4*>(out)[lane] = any ? make_float4(o.x / l, o.y / l, o.z / l, o.w / l) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
+    __device__ __forceinline__ void finish(unsigned short* out, int lane) const {
+        const float r = l > 0.f ? 1.f / l : 0.f;
+        reinterpret_cast<uint2*>(out)[lane] = make_uint2(pack_bf2(o.x * r, o.y * r), pack_bf2(o.z * r, o.w * r));
+    }
 };
 
 // Merge of the heads that several warps share, at the end of the main kernel.  First the shares of this CTA's warps (at most one
@@ -659,8 +680,8 @@ struct MergedState {
 // those, the CTA that arrives last at the query head's counter merges the CTAs' states, in CTA order, and writes the output: no
 // CTA waits for another, and the result does not depend on which one is last.  What this costs is latency, most of it the
 // release before the counters (1.3 us, 4.7 us when all CTAs get there together), so the CTA's counters are advanced together.
-template <int MAIN_WARPS>
-__device__ __forceinline__ void merge_shared_heads(const DecodeParams& P, const SharedHead* shared_s, const long long total) {
+template <int MAIN_WARPS, class Out>
+__device__ __forceinline__ void merge_shared_heads(const DecodeParams& P, Out* outputs, const SharedHead* shared_s, const long long total) {
     const CacheView& c = P.c;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, G = c.G;
     __shared__ int leader_s[2], n_ctas_s[2], last_s[2][8];       // [0] the CTA's first shared head, [1] its last one if that is another
@@ -694,7 +715,7 @@ __device__ __forceinline__ void merge_shared_heads(const DecodeParams& P, const 
             if (lane == 0) { leader_s[k_head == 0 ? 0 : 1] = leader; n_ctas_s[k_head == 0 ? 0 : 1] = n_ctas; }
         }
         if (n_ctas > 1) ms.store(P.part + (static_cast<long long>(hd.bh) * G + head) * PART_STRIDE + (cta_warp0 + (leader >> 1)) * rec_step, lane);
-        else ms.finish(P.O + (static_cast<long long>(hd.bh / c.n_kv) * c.n_q + (hd.bh % c.n_kv) * G + head) * D, lane);
+        else ms.finish(outputs + (static_cast<long long>(hd.bh / c.n_kv) * c.n_q + (hd.bh % c.n_kv) * G + head) * D, lane);
     }
     __syncthreads();
     const int n_ends = n_heads > 1 ? 2 : 1;
@@ -724,7 +745,7 @@ __device__ __forceinline__ void merge_shared_heads(const DecodeParams& P, const 
                 const long long u = every_cta ? max(hd.first, static_cast<long long>(c_first + k) * MAIN_WARPS * total / P.n_warps) : hd.first + k;
                 return rec0 + slice_owner(u, total, P.n_warps) * rec_step;
             });
-        ms.finish(P.O + (static_cast<long long>(hd.bh / c.n_kv) * c.n_q + (hd.bh % c.n_kv) * G + head) * D, lane);
+        ms.finish(outputs + (static_cast<long long>(hd.bh / c.n_kv) * c.n_q + (hd.bh % c.n_kv) * G + head) * D, lane);
     }
 }
 
@@ -742,8 +763,23 @@ __device__ __forceinline__ unsigned long long gtime() { unsigned long long t; as
 #define TL(slot) do { } while (0)
 #endif
 
-template <int BITS, int MODE, int STAGES>
+// Outputs of dense or sparse attention.
+template <bool SPARSE> struct OutputOf;
+template <> struct OutputOf<false> { using type = float; static __device__ __forceinline__ float* of(const DecodeParams& P) { return P.O; } };
+template <> struct OutputOf<true> { using type = unsigned short; static __device__ __forceinline__ unsigned short* of(const DecodeParams& P) { return P.O16; } };
+
+// SPARSE: the packed pages of a (sequence, KV head) are those of its list instead of all; the list is written by the selection
+// kernel ahead of this one, so nothing is staged before that has ended.  A warp has few units here (16 sequences x 8 heads x
+// (64 pages + 17 window units) are 4.4 units for each of 2368 warps), so the two dependent loads list -> page table of a unit
+// would cost as much as the unit: the lanes make them for 32 units of a round at once.
+template <int BITS, int MODE, int STAGES, bool SPARSE>
 __global__ void __launch_bounds__(main_warps(BITS, MODE) * 32, 1) decode_main_kernel(DecodeParams P) {
+    using Out = typename OutputOf<SPARSE>::type;
+    Out* const outputs = OutputOf<SPARSE>::of(P);
+    const auto info = [&](int b) {
+        const SeqInfo si = seq_info(P.c, __ldcg(P.seq_len + b), __ldg(P.slot + b));
+        return SPARSE ? sparse_info(si, P.n_select) : si;
+    };
     constexpr int MAIN_WARPS = main_warps(BITS, MODE);
     constexpr int REC = record_bytes(BITS);
     constexpr int CB = code_block_bytes(BITS);
@@ -765,7 +801,7 @@ __global__ void __launch_bounds__(main_warps(BITS, MODE) * 32, 1) decode_main_ke
     long long* plan_s = reinterpret_cast<long long*>(smem);
     static_assert((MAX_LOCAL_PLAN + 1) * sizeof(long long) <= static_cast<size_t>(MAIN_WARPS) * STAGES * REC, "the plan must fit in the staging area");
     const bool local_plan = P.batch <= MAX_LOCAL_PLAN;
-    if (P.q_early || !local_plan) pdl_wait();           // lengths from the append / plan from the preparation kernel
+    if (P.q_early || !local_plan || SPARSE) pdl_wait();  // lengths from the append / plan from the preparation kernel / list from the selection kernel
     for (int b = blockIdx.x * MAIN_WARPS * 32 + threadIdx.x; b < P.batch; b += gridDim.x * MAIN_WARPS * 32) {
         const int slot = __ldg(P.slot + b);
         if (slot < 0 || slot >= c.n_slots) atomicOr(c.dev_status, WUSHKV_DEV_BAD_SLOT);
@@ -775,7 +811,7 @@ __global__ void __launch_bounds__(main_warps(BITS, MODE) * 32, 1) decode_main_ke
         for (int base = 0; base < P.batch; base += MAIN_WARPS * 32) {
             const int bb = base + threadIdx.x;
             long long incl = 0;
-            if (bb < P.batch) incl = seq_info(c, __ldcg(P.seq_len + bb), __ldg(P.slot + bb)).U;
+            if (bb < P.batch) incl = info(bb).U;
             for (int o = 1; o < 32; o <<= 1) {
                 const long long v = __shfl_up_sync(FULL, incl, o);
                 if (lane >= o) incl += v;
@@ -815,7 +851,7 @@ __global__ void __launch_bounds__(main_warps(BITS, MODE) * 32, 1) decode_main_ke
     }
     for (int b = blockIdx.x; b < P.batch; b += gridDim.x)      // a sequence without units gets zeros
         if (plan[b + 1] == plan[b])
-            for (int k = threadIdx.x; k < c.n_q * D; k += MAIN_WARPS * 32) P.O[static_cast<long long>(b) * c.n_q * D + k] = 0.f;
+            for (int k = threadIdx.x; k < c.n_q * D; k += MAIN_WARPS * 32) put_output(outputs + static_cast<long long>(b) * c.n_q * D + k, 0.f);
     __shared__ SharedHead shared_s[2 * MAIN_WARPS];             // [2 warp]: head the warp entered in its middle, [2 warp + 1]: head it left unfinished
     __shared__ long long total_s;           // kept for the merge at the end
     if (threadIdx.x < 2 * MAIN_WARPS) shared_s[threadIdx.x].bh = -1;
@@ -850,7 +886,7 @@ __global__ void __launch_bounds__(main_warps(BITS, MODE) * 32, 1) decode_main_ke
         // ================= round set-up: list the next segments of the slice =====================
         int n_seg = 0, round_units = 0;
         while (n_seg < MAX_SEGMENTS && L < L1) {
-            const SeqInfo si = seq_info(c, __ldcg(P.seq_len + sb), __ldg(P.slot + sb));
+            const SeqInfo si = info(sb);
             if (si.U > 0) {
                 const int u1 = static_cast<int>(min(static_cast<long long>(si.U), su + (L1 - L)));
                 if (lane == 0) {
@@ -877,24 +913,52 @@ __global__ void __launch_bounds__(main_warps(BITS, MODE) * 32, 1) decode_main_ke
         const long long round_L0 = L - round_units;      // flattened index of the round's first unit
         int p_seg = -1, p_u = 0, p_u1 = 0, p_qp = 0, p_head_off = 0, issued = 0;
         const int* p_ptab = nullptr;
+        // SPARSE: list entry and page of the round's units [32 k, 32 k + 32), a lane each (-1: not a page of the list, -2: a bad one)
+        int l_entry = -1, l_page = -1;
+        auto look_up = [&](int first_unit) {
+            const int u = first_unit + lane;
+            l_entry = l_page = -1;
+            int seg = 0, before = 0;
+            while (seg < n_seg - 1 && u - before >= segs[seg].u1 - segs[seg].u0) { before += segs[seg].u1 - segs[seg].u0; ++seg; }
+            const Segment& sg = segs[seg];
+            const int k = sg.u0 + u - before;
+            if (u < round_units && k < sg.qp) {
+                const int e = __ldcg(P.selected + (static_cast<long long>(sg.b) * c.n_kv + sg.h) * P.n_select + k);
+                if (e >= 0) {
+                    const bool inside = e >= sg.first_page && e < c.max_pages && static_cast<long long>(e) * PAGE_TOKENS < sg.q_hi;
+                    const int page = inside ? __ldcg(c.page_table + static_cast<long long>(sg.slot) * c.max_pages + e) : -1;
+                    l_entry = e;
+                    l_page = static_cast<unsigned>(page) < static_cast<unsigned long long>(c.n_pages) ? page : -2;
+                }
+            }
+        };
+        int entry_a = 0, entry_b = 0;                   // SPARSE: list entries of the units in stages 0 and 1
+        static_assert(!SPARSE || STAGES == 2, "one list entry per stage");
         auto issue_next = [&](const int s) {            // whole warp; stages the round's next unit into ring slot s
             if (p_u == p_u1) {                          // next segment
                 ++p_seg;
                 const Segment& sg = segs[p_seg];
                 p_u = sg.u0; p_u1 = sg.u1; p_qp = sg.qp; p_head_off = sg.h * REC;
                 p_ptab = c.page_table + static_cast<long long>(sg.slot) * c.max_pages + sg.first_page;
-                if (sg.first_page + sg.qp > c.max_pages) {      // the page table cannot hold this length
+                if (!SPARSE && sg.first_page + sg.qp > c.max_pages) {      // the page table cannot hold this length
                     if (lane == 0) atomicOr(c.dev_status, WUSHKV_DEV_PAGE_TABLE_FULL);
                     p_qp = min(p_qp, max(c.max_pages - sg.first_page, 0));   // pages beyond it are treated as window-less gaps below
                 }
             }
             const unsigned bar = bar0 + 8 * s, dst = stage0 + s * REC;
             const Segment& sg = segs[p_seg];
+            int sparse_page = -1;
+            if (SPARSE) {
+                if ((issued & 31) == 0) look_up(issued);
+                const int entry = __shfl_sync(FULL, l_entry, issued & 31);
+                sparse_page = __shfl_sync(FULL, l_page, issued & 31);
+                if (s == 0) entry_a = entry; else entry_b = entry;
+            }
             if (p_u < sg.qp) {                          // a packed page: one bulk copy
                 if (lane == 0) {
-                    const int page = (p_u < p_qp) ? __ldg(p_ptab + p_u) : -1;
+                    const int page = SPARSE ? sparse_page : (p_u < p_qp) ? __ldg(p_ptab + p_u) : -1;
                     if (static_cast<unsigned>(page) >= static_cast<unsigned long long>(c.n_pages)) {
-                        if (p_u < p_qp) atomicOr(c.dev_status, WUSHKV_DEV_BAD_PAGE_ID);
+                        if (SPARSE ? page != -1 : p_u < p_qp) atomicOr(c.dev_status, WUSHKV_DEV_BAD_PAGE_ID);
                         bad_bits |= 1u << s;
                         mbar_arrive(bar);
                     } else if (WUSHKV_ABL & 8) {        // timing experiment: no copy, the stage keeps its (zeroed) content
@@ -983,6 +1047,7 @@ __global__ void __launch_bounds__(main_warps(BITS, MODE) * 32, 1) decode_main_ke
                     window_unit<BITS, MODE>(st, rec, min(WIN_TOKENS, sg.n_win - w0),
                                             P.qwfrag + (static_cast<long long>(sg.b) * c.n_kv + sg.h) * 256, lane);
                 } else if (!__any_sync(FULL, (bad_bits >> s) & 1u)) {
+                    if (SPARSE) pos0 = (s == 0 ? entry_a : entry_b) * PAGE_TOKENS;
                     // ======================= packed page: 64 quantized tokens ==========================
                     const bool full_page = (pos0 >= q_lo) && (pos0 + PAGE_TOKENS <= q_hi);
                     float sc[4][2 * NH];          // [block][row g: heads..., row g+8: heads...]
@@ -1159,7 +1224,7 @@ __global__ void __launch_bounds__(main_warps(BITS, MODE) * 32, 1) decode_main_ke
             // the warp's ring if that has served its last unit, else in global memory.
             const int U = qp + (sg.n_win + WIN_TOKENS - 1) / WIN_TOKENS;
             if (sg.u0 == 0 && u1 == U) {
-                store_state<BITS, MODE, true>(st, P.O + (static_cast<long long>(sg.b) * c.n_q + sg.h * G) * D, lane, G);
+                store_state<BITS, MODE, true>(st, outputs + (static_cast<long long>(sg.b) * c.n_q + sg.h * G) * D, lane, G);
             } else {
                 static_assert(8 * PART_STRIDE * 4 <= STAGES * REC, "the partials of 8 query heads must fit in a warp's ring");
                 const bool last = cs == n_seg - 1 && L >= L1;
@@ -1178,7 +1243,7 @@ __global__ void __launch_bounds__(main_warps(BITS, MODE) * 32, 1) decode_main_ke
     // ---- heads that several warps share
     pdl_wait();                             // warps without units: the counters were zeroed by the preparation kernel
     __syncthreads();
-    merge_shared_heads<MAIN_WARPS>(P, shared_s, total_s);
+    merge_shared_heads<MAIN_WARPS>(P, outputs, shared_s, total_s);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -1191,9 +1256,11 @@ struct DecodePlan {
 
 static size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
-static bool make_plan(const CacheView& c, int batch, int max_seq_len, DecodePlan& pl) {
+// n_select > 0: sparse attention over at most that many packed pages
+static bool make_plan(const CacheView& c, int batch, int max_seq_len, DecodePlan& pl, int n_select = 0) {
     if (batch <= 0 || max_seq_len <= 0) return false;
-    const long long pages_max = (static_cast<long long>(max_seq_len) + PAGE_TOKENS - 1) / PAGE_TOKENS + 1;
+    long long pages_max = (static_cast<long long>(max_seq_len) + PAGE_TOKENS - 1) / PAGE_TOKENS + 1;
+    if (n_select > 0) pages_max = std::min<long long>(pages_max, n_select);
     const long long win_max = std::min<long long>(max_seq_len, c.s_sink + c.s_keep + c.s_flush - 1 + c.lag);
     const long long units_max = (pages_max + (win_max + WIN_TOKENS - 1) / WIN_TOKENS + 1) * batch * c.n_kv;
     const int warps = main_warps(c.bits, c.G <= 4 ? 0 : 1);
@@ -1218,8 +1285,9 @@ static bool make_plan(const CacheView& c, int batch, int max_seq_len, DecodePlan
 
 static cudaEvent_t g_prof_start = nullptr, g_prof_stop = nullptr;
 
-template <int BITS, int MODE>
-static int launch_decode(const DecodeParams& P, int n_ctas, cudaStream_t st) {
+// selection: the kernel that fills P.selected goes between the preparation and the main kernel
+template <int BITS, int MODE, bool SPARSE>
+static int launch_decode(const DecodeParams& P, int n_ctas, cudaStream_t st, const SelectParams* selection, int max_seq_len) {
     constexpr int MAIN_WARPS = main_warps(BITS, MODE);
 #ifndef WUSHKV_STAGES_2BIT
 #define WUSHKV_STAGES_2BIT 2
@@ -1238,12 +1306,16 @@ static int launch_decode(const DecodeParams& P, int n_ctas, cudaStream_t st) {
     cfg.blockDim = dim3(PREP_THREADS);
     cfg.dynamicSmemBytes = 0;
     if (cudaLaunchKernelEx(&cfg, decode_prep_kernel<BITS, MODE>, P) != cudaSuccess) return WUSHKV_ECUDA;
-    if (!opt_in_dynamic_smem(reinterpret_cast<const void*>(decode_main_kernel<BITS, MODE, STAGES>), static_cast<int>(SMEM))) return WUSHKV_ECUDA;
+    if (SPARSE && selection) {
+        const int rc = launch_select(*selection, max_seq_len, st);
+        if (rc != WUSHKV_OK) return rc;
+    }
+    if (!opt_in_dynamic_smem(reinterpret_cast<const void*>(decode_main_kernel<BITS, MODE, STAGES, SPARSE>), static_cast<int>(SMEM))) return WUSHKV_ECUDA;
     if (g_prof_start) cudaEventRecord(g_prof_start, st);
     cfg.gridDim = dim3(n_ctas);
     cfg.blockDim = dim3(MAIN_WARPS * 32);
     cfg.dynamicSmemBytes = SMEM;
-    if (cudaLaunchKernelEx(&cfg, decode_main_kernel<BITS, MODE, STAGES>, P) != cudaSuccess) return WUSHKV_ECUDA;
+    if (cudaLaunchKernelEx(&cfg, decode_main_kernel<BITS, MODE, STAGES, SPARSE>, P) != cudaSuccess) return WUSHKV_ECUDA;
     if (g_prof_stop) cudaEventRecord(g_prof_stop, st);
     return WUSHKV_OK;
 }
@@ -1260,17 +1332,30 @@ extern "C" size_t wushkv_decode_workspace_bytes(const wushkv_cache* cache, int32
     return pl.total;
 }
 
+// What sparse attention adds to a call: the list of pages and, where the call makes it itself, what it is made from.
+struct SparseArgs {
+    int n_select;
+    int* selected;
+    const int8_t* bounds;        // nullptr: the list is an input
+    const int8_t* exponents;
+    uint16_t* O16;
+};
+
 static int decode_attn_impl(const wushkv_cache* cache, int32_t batch, const int32_t* slot, const int32_t* seq_len,
                             int32_t max_seq_len, const uint16_t* Q, float* O,
                             void* workspace, size_t workspace_bytes, void* stream, int q_early,
-                            const wushkv_prologue* prologue = nullptr) {
+                            const wushkv_prologue* prologue = nullptr, const SparseArgs* sparse = nullptr) {
     DecodeParams P;
     P.q_early = q_early;
     const int rc = make_view(cache, P.c);
     if (rc != WUSHKV_OK) return rc;
-    if (!slot || !seq_len || !Q || !O || !workspace || !aligned(Q, 16) || !aligned(O, 16) || !aligned(workspace, 256)) return WUSHKV_EINVAL;
+    const void* out = sparse ? static_cast<const void*>(sparse->O16) : O;
+    if (!slot || !seq_len || !Q || !out || !workspace || !aligned(Q, 16) || !aligned(out, 16) || !aligned(workspace, 256)) return WUSHKV_EINVAL;
+    if (sparse && (sparse->n_select <= 0 || !sparse->selected || (sparse->bounds == nullptr) != (sparse->exponents == nullptr) || !aligned(sparse->bounds, 16)))
+        return WUSHKV_EINVAL;
     DecodePlan pl;
-    if (!make_plan(P.c, batch, max_seq_len, pl)) return WUSHKV_EINVAL;
+    if (!make_plan(P.c, batch, max_seq_len, pl, sparse ? sparse->n_select : 0)) return WUSHKV_EINVAL;
+    if (sparse && sparse->bounds && candidate_bound(P.c, max_seq_len) > MAX_SELECT_PAGES) return WUSHKV_ECAPACITY;
     if (batch > 65535) return WUSHKV_EINVAL;
     if (workspace_bytes < pl.total) return WUSHKV_ECAPACITY;
     unsigned char* ws = static_cast<unsigned char*>(workspace);
@@ -1285,6 +1370,9 @@ static int decode_attn_impl(const wushkv_cache* cache, int32_t batch, const int3
     P.drop_unit = knobs().drop_copy_unit;
     P.pro = Prologue{nullptr, 0, 0, nullptr, 0.f};
     if (prologue && !make_prologue(prologue, prologue->q_norm_weight, P.pro)) return WUSHKV_EINVAL;
+    P.selected = sparse ? sparse->selected : nullptr;
+    P.n_select = sparse ? sparse->n_select : 0;
+    P.O16 = sparse ? sparse->O16 : nullptr;
     {   // upper bound of the packed bytes one step reads against the L2 size
         static int l2_bytes[64] = {};
         int dev = 0;
@@ -1294,15 +1382,53 @@ static int decode_attn_impl(const wushkv_cache* cache, int32_t batch, const int3
             if (cudaDeviceGetAttribute(&l2, cudaDevAttrL2CacheSize, dev) != cudaSuccess) return WUSHKV_ECUDA;
             if (dev >= 0 && dev < 64) l2_bytes[dev] = l2;
         }
-        const double step_bytes = static_cast<double>(batch) * P.c.n_kv * ((max_seq_len + PAGE_TOKENS - 1) / PAGE_TOKENS) *
-                                  record_bytes(P.c.bits);
+        double step_pages = (max_seq_len + PAGE_TOKENS - 1) / PAGE_TOKENS;
+        if (sparse) step_pages = std::min<double>(step_pages, sparse->n_select);
+        const double step_bytes = static_cast<double>(batch) * P.c.n_kv * step_pages * record_bytes(P.c.bits);
         P.stream_pages = step_bytes > static_cast<double>(l2) ? 1 : 0;
     }
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool mode0 = P.c.G <= 4;
-    if (P.c.bits == 2) return mode0 ? launch_decode<2, 0>(P, pl.n_ctas, st) : launch_decode<2, 1>(P, pl.n_ctas, st);
-    if (P.c.bits == 3) return mode0 ? launch_decode<3, 0>(P, pl.n_ctas, st) : launch_decode<3, 1>(P, pl.n_ctas, st);
-    return mode0 ? launch_decode<4, 0>(P, pl.n_ctas, st) : launch_decode<4, 1>(P, pl.n_ctas, st);
+    if (sparse) {
+        SelectParams sel = {};
+        if (sparse->bounds) {
+            sel.c = P.c; sel.batch = batch; sel.slot = slot; sel.seq_len = seq_len; sel.Q = Q; sel.pro = P.pro;
+            sel.bounds = reinterpret_cast<const signed char*>(sparse->bounds);
+            sel.exponents = reinterpret_cast<const signed char*>(sparse->exponents);
+            sel.n_select = sparse->n_select; sel.selected = sparse->selected;
+            sel.early = 1;       // every CTA of the preparation kernel has waited for all earlier work when this one may start
+        }
+        const SelectParams* selection = sparse->bounds ? &sel : nullptr;
+        if (P.c.bits == 2) return mode0 ? launch_decode<2, 0, true>(P, pl.n_ctas, st, selection, max_seq_len) : launch_decode<2, 1, true>(P, pl.n_ctas, st, selection, max_seq_len);
+        if (P.c.bits == 3) return mode0 ? launch_decode<3, 0, true>(P, pl.n_ctas, st, selection, max_seq_len) : launch_decode<3, 1, true>(P, pl.n_ctas, st, selection, max_seq_len);
+        return mode0 ? launch_decode<4, 0, true>(P, pl.n_ctas, st, selection, max_seq_len) : launch_decode<4, 1, true>(P, pl.n_ctas, st, selection, max_seq_len);
+    }
+    if (P.c.bits == 2) return mode0 ? launch_decode<2, 0, false>(P, pl.n_ctas, st, nullptr, 0) : launch_decode<2, 1, false>(P, pl.n_ctas, st, nullptr, 0);
+    if (P.c.bits == 3) return mode0 ? launch_decode<3, 0, false>(P, pl.n_ctas, st, nullptr, 0) : launch_decode<3, 1, false>(P, pl.n_ctas, st, nullptr, 0);
+    return mode0 ? launch_decode<4, 0, false>(P, pl.n_ctas, st, nullptr, 0) : launch_decode<4, 1, false>(P, pl.n_ctas, st, nullptr, 0);
+}
+
+extern "C" size_t wushkv_sparse_workspace_bytes(const wushkv_cache* cache, int32_t batch, int32_t max_seq_len, int32_t n_select) {
+    CacheView v;
+    if (make_view(cache, v) != WUSHKV_OK || n_select <= 0) return 0;
+    DecodePlan pl;
+    if (!make_plan(v, batch, max_seq_len, pl, n_select)) return 0;
+    return pl.total;
+}
+
+extern "C" int wushkv_decode_attn_selected(const wushkv_cache* cache, int32_t batch, const int32_t* slot, const int32_t* seq_len, int32_t max_seq_len,
+                                           const uint16_t* Q, const wushkv_prologue* prologue, const int32_t* selected, int32_t n_select, uint16_t* O,
+                                           void* workspace, size_t workspace_bytes, void* stream) {
+    const SparseArgs sparse = {n_select, const_cast<int32_t*>(selected), nullptr, nullptr, O};
+    return decode_attn_impl(cache, batch, slot, seq_len, max_seq_len, Q, nullptr, workspace, workspace_bytes, stream, 0, prologue, &sparse);
+}
+
+extern "C" int wushkv_decode_attn_sparse(const wushkv_cache* cache, int32_t batch, const int32_t* slot, const int32_t* seq_len, int32_t max_seq_len,
+                                         const uint16_t* Q, const wushkv_prologue* prologue, const int8_t* bounds, const int8_t* exponents,
+                                         int32_t n_select, int32_t* selected, uint16_t* O, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!bounds || !exponents) return WUSHKV_EINVAL;
+    const SparseArgs sparse = {n_select, selected, bounds, exponents, O};
+    return decode_attn_impl(cache, batch, slot, seq_len, max_seq_len, Q, nullptr, workspace, workspace_bytes, stream, 0, prologue, &sparse);
 }
 
 extern "C" int wushkv_decode_attn(const wushkv_cache* cache, int32_t batch, const int32_t* slot, const int32_t* seq_len,

@@ -1,0 +1,515 @@
+// Bounds of packed pages and the selection of pages by them (the attention over the selected pages is in decode.cu).
+//
+// A page and head keeps, beside its packed record, 257 bytes: for every channel the smallest and the largest dequantized key
+// of the page's tokens, rounded outwards to multiples of a power of two that is common to the page and head,
+//     e = least integer >= -31 with max |khat| <= 127 * 2^e,  lower = floor(min khat / 2^e),  upper = ceil(max khat / 2^e).
+// With them the largest score that any token of the page can reach against a query q' is
+//     2^e * sum_c ( max(q'_c, 0) upper_c + min(q'_c, 0) lower_c ),
+// a dot product of 256 terms.  The query enters as 16-bit fixed point (two signed bytes per channel), so that the sum is an
+// exact integer from mma.sync.m16n8k32 (s8 x s8): scores, and with them the selected pages, do not depend on the order of any
+// summation.  q' itself is formed in 64 bits for the same reason: its rounding to 16 bits then is the same wherever it is done.
+#include <cooperative_groups.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+
+#include "host_common.h"
+#include "sparse.cuh"
+
+namespace wushkv {
+
+namespace cg = cooperative_groups;
+
+constexpr unsigned FULL = 0xffffffffu;
+constexpr int MIN_EXPONENT = -31, MAX_EXPONENT = 14;      // of 2^e: fp16 steps and offsets reach from 2^-24 to 2^20
+constexpr double Q_MAX = 32512.0;                         // 127 * 256: both digits of the fixed-point query fit a signed byte
+
+// ------------------------------------------------------------------------------------------------
+// bounds
+// ------------------------------------------------------------------------------------------------
+struct BoundsParams {
+    CacheView c;
+    const int* slot;
+    const int* seq_len;
+    const int* cu_new;
+    signed char* bounds;
+    signed char* exponents;
+};
+
+// Halves the live values of a butterfly over one lane bit: afterwards v[0 .. N) hold the lane's half, combined.
+template <int N, bool MAX>
+__device__ __forceinline__ void halve(float* v, int lane, int bit) {
+    const bool upper = (lane & bit) != 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float send = upper ? v[i] : v[i + N], keep = upper ? v[i + N] : v[i];
+        const float got = __shfl_xor_sync(FULL, send, bit);
+        v[i] = MAX ? fmaxf(keep, got) : fminf(keep, got);
+    }
+}
+
+// A warp per (page, head).  Lane (g, t) reads the code words of token rows g and g + 8 of every 16-token block, which hold the
+// channels 32 s + 16 hh + 8 u + 2 t + v of all s, hh, u, v: 32 running minima and maxima per lane, combined over g at the end.
+template <int BITS>
+__global__ void __launch_bounds__(256) page_bounds_kernel(BoundsParams P) {
+    constexpr int REC = record_bytes(BITS), CB = code_block_bytes(BITS);
+    const CacheView& c = P.c;
+    const int b = blockIdx.y, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int unit = blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int len = P.seq_len[b], n = P.cu_new[b + 1] - P.cu_new[b], slot = P.slot[b];
+    if (n <= 0 || len <= 0) return;
+    if (slot < 0 || slot >= c.n_slots) { if (unit == 0 && lane == 0) atomicOr(c.dev_status, WUSHKV_DEV_BAD_SLOT); return; }
+    const int index = max(len - n, 0) / PAGE_TOKENS + unit / c.n_kv, h = unit % c.n_kv;
+    if (index > (len - 1) / PAGE_TOKENS) return;
+    if (index >= c.max_pages) { if (lane == 0) atomicOr(c.dev_status, WUSHKV_DEV_PAGE_TABLE_FULL); return; }
+    const int page = c.page_table[static_cast<long long>(slot) * c.max_pages + index];
+    if (page < 0 || page >= c.n_pages) { if (lane == 0) atomicOr(c.dev_status, WUSHKV_DEV_BAD_PAGE_ID); return; }
+    const long long ph = static_cast<long long>(page) * c.n_kv + h;
+    const unsigned char* rec = c.pages + ph * REC;
+
+    uint4 words[4][BITS == 4 ? 2 : 1], meta[4];
+    uint2 high[4];
+#pragma unroll
+    for (int bi = 0; bi < 4; ++bi) {
+#pragma unroll
+        for (int p = 0; p < (BITS == 4 ? 2 : 1); ++p) words[bi][p] = __ldg(reinterpret_cast<const uint4*>(rec + bi * CB + 512 * p) + lane);
+        if (BITS == 3) high[bi] = __ldg(reinterpret_cast<const uint2*>(rec + k_hi_offset(3) + bi * 256) + lane);
+        meta[bi] = __ldg(reinterpret_cast<const uint4*>(rec + meta_offset(BITS) + 128 * bi) + g);
+    }
+    float lo[32], hi[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) { lo[j] = INFINITY; hi[j] = -INFINITY; }
+#pragma unroll
+    for (int bi = 0; bi < 4; ++bi) {
+        float step[2], low[2];
+#pragma unroll
+        for (int rs = 0; rs < 2; ++rs) {
+            const unsigned m = rs == 0 ? meta[bi].x : meta[bi].z;
+            __half2 h2;
+            *reinterpret_cast<unsigned*>(&h2) = m;
+            const float2 f = __half22float2(h2);
+            const bool there = index * PAGE_TOKENS + 16 * bi + 8 * rs + g < len;
+            step[rs] = there ? f.x : 0.f;
+            low[rs] = there ? f.y : NAN;                 // minimum and maximum pass over a NaN: a token that is not there, or a damaged one
+        }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+#pragma unroll
+                for (int by = 0; by < 4; ++by) {
+                    float v[2];
+#pragma unroll
+                    for (int rs = 0; rs < 2; ++rs) {
+                        const uint4& q = words[bi][BITS == 4 ? s >> 1 : 0];
+                        const unsigned w = hh == 0 ? (rs == 0 ? q.x : q.y) : (rs == 0 ? q.z : q.w);
+                        unsigned code = BITS == 4 ? (w >> (8 * by + 4 * (s & 1))) & 15u : (w >> (8 * by + 2 * s)) & 3u;
+                        if (BITS == 3) code |= (((rs == 0 ? high[bi].x : high[bi].y) >> (8 * by + 2 * s + hh)) & 1u) << 2;
+                        // step * code has at most 15 bits: the multiply-add rounds once, as the sum alone does
+                        v[rs] = fmaf(step[rs], static_cast<float>(code), low[rs]);
+                    }
+                    const int j = 8 * s + 4 * hh + by;
+                    lo[j] = fminf(lo[j], fminf(v[0], v[1]));
+                    hi[j] = fmaxf(hi[j], fmaxf(v[0], v[1]));
+                }
+            }
+        }
+    }
+    halve<16, false>(lo, lane, 16); halve<16, true>(hi, lane, 16);
+    halve<8, false>(lo, lane, 8);   halve<8, true>(hi, lane, 8);
+    halve<4, false>(lo, lane, 4);   halve<4, true>(hi, lane, 4);
+    float most = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) most = fmaxf(most, fmaxf(fabsf(lo[i]), fabsf(hi[i])));
+    const unsigned bits = __reduce_max_sync(FULL, __float_as_uint(most));          // magnitudes compare like their bits
+    int e = static_cast<int>(bits >> 23) - 126;                                       // most = f * 2^e, 1/2 <= f < 1
+    e -= (bits & 0x7fffffu) <= 0x7e0000u ? 7 : 6;                                     // f <= 127/128 or not
+    e = min(max(e, MIN_EXPONENT), MAX_EXPONENT);
+    const float scale = __uint_as_float(static_cast<unsigned>(127 - e) << 23);
+    int ql[4], qh[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        ql[i] = min(max(__float2int_rd(lo[i] * scale), -127), 127);
+        qh[i] = min(max(__float2int_ru(hi[i] * scale), -127), 127);
+    }
+    // lane bits 4, 3, 2 chose j's bits 4, 3, 2, i is by = 2 u + v: channels ch, ch + 1, ch + 8, ch + 9
+    const int j0 = 16 * (lane >> 4) + 8 * ((lane >> 3) & 1) + 4 * ((lane >> 2) & 1);
+    const int ch = 32 * (j0 >> 3) + 16 * ((j0 >> 2) & 1) + 2 * t;
+    unsigned short* out = reinterpret_cast<unsigned short*>(P.bounds + ph * 2 * D);
+    const auto pair = [](int a, int b2) { return static_cast<unsigned short>((a & 255) | ((b2 & 255) << 8)); };
+    out[ch / 2] = pair(ql[0], ql[1]);
+    out[ch / 2 + 4] = pair(ql[2], ql[3]);
+    out[D / 2 + ch / 2] = pair(qh[0], qh[1]);
+    out[D / 2 + ch / 2 + 4] = pair(qh[2], qh[3]);
+    if (lane == 0) P.exponents[ph] = static_cast<signed char>(e);
+}
+
+// ------------------------------------------------------------------------------------------------
+// selection
+// ------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void mma_s8(int (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+constexpr int SELECT_THREADS = 256, SELECT_WARPS = SELECT_THREADS / 32;
+
+// Shared memory of a CTA: fixed part, then the scores of its pages [heads][per], then (CTA 0) the keys of all pages.
+struct SelectShared {
+    double q[8][D];                   // the queries, in 64 bits
+    double qc[8][D];                  // q' of all CTAs' rows
+    uint4 frag[2 * 4 * 32];           // B fragments: [digit set][64 bytes of bounds][lane]
+    float unit[8];                    // score of one unit of 2^e dot
+    float warp_best[SELECT_WARPS][8];
+    float best[16][8];                // per CTA of the cluster: largest score of its pages, per head
+    int count[SELECT_WARPS];
+    int scan[SELECT_WARPS];
+};
+
+__host__ __device__ inline int pages_per_cta(int pages, int cl) { return ((pages + cl - 1) / cl + 15) / 16 * 16; }
+
+// One cluster of CL CTAs per (sequence, KV head).
+//   1. q' = T_K^{-T} q: each CTA forms 128 / CL rows of it and hands them to the others through distributed shared memory.
+//   2. Each CTA scores its share of the pages, 16 pages per warp and step: bounds straight from global memory into the A
+//      fragments (their bytes are consecutive in k, so that one 16-byte load per lane and row is two registers of two k-steps).
+//   3. The largest score per head of all CTAs, the key of every page (how far it is below the best page of the head that it
+//      matters most to), sent to CTA 0.
+//   4. CTA 0 finds the n_select-th largest key bit by bit and lists the pages.
+// All of it is latency: the bounds of 16 sequences x 8 heads x 510 pages are 17 MB, 2.6 us at the copy rate.
+template <int MODE, int CL>
+__global__ void __launch_bounds__(SELECT_THREADS) select_pages_kernel(SelectParams P) {
+    constexpr int GP = MODE == 0 ? 4 : 8, SETS = MODE == 0 ? 1 : 2;
+    extern __shared__ __align__(16) unsigned char select_smem[];
+    SelectShared& sh = *reinterpret_cast<SelectShared*>(select_smem);
+    cg::cluster_group cluster = cg::this_cluster();
+    const CacheView& c = P.c;
+    const int rank = static_cast<int>(cluster.block_rank()), h = blockIdx.y, b = blockIdx.z;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3, G = c.G;
+    if (!P.early) pdl_wait();
+    pdl_launch_dependents();
+    if (CL > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");       // the other CTAs' shared memory exists once they have arrived
+
+    // ---- candidates
+    const int S = __ldcg(P.seq_len + b), slot = P.slot[b];
+    int* out = P.selected + (static_cast<long long>(b) * c.n_kv + h) * P.n_select;
+    int pages = 0, first = 0;
+    if (slot < 0 || slot >= c.n_slots) {
+        if (rank == 0 && h == 0 && tid == 0) atomicOr(c.dev_status, WUSHKV_DEV_BAD_SLOT);
+    } else if (S > 0) {
+        const int nq = n_quantized(S - c.lag, c.s_sink, c.s_keep, c.s_flush);
+        first = c.s_sink / PAGE_TOKENS;
+        pages = nq > 0 ? (c.s_sink + nq - 1) / PAGE_TOKENS - first + 1 : 0;
+        if (first + pages > c.max_pages) {
+            if (rank == 0 && h == 0 && tid == 0) atomicOr(c.dev_status, WUSHKV_DEV_PAGE_TABLE_FULL);
+            pages = max(c.max_pages - first, 0);
+        }
+        if (pages > P.max_candidates) {                 // a sequence longer than promised
+            if (rank == 0 && h == 0 && tid == 0) atomicOr(c.dev_status, WUSHKV_DEV_BAD_COUNT);
+            pages = P.max_candidates;
+        }
+    }
+    const bool all = pages <= P.n_select;               // the same for the whole cluster
+    if (all) {
+        if (rank == 0)
+            for (int i = tid; i < P.n_select; i += SELECT_THREADS) out[i] = i < pages ? first + i : -1;
+        if (CL > 1) asm volatile("barrier.cluster.wait;" ::: "memory");
+        if (P.early) pdl_wait();
+        return;
+    }
+    const int per_max = pages_per_cta(P.max_candidates, CL);
+    float* scores = reinterpret_cast<float*>(select_smem + sizeof(SelectShared));            // [G][per_max]
+    unsigned* keys = reinterpret_cast<unsigned*>(scores + static_cast<size_t>(G) * per_max);
+    const int per = pages_per_cta(pages, CL), p_lo = min(rank * per, pages), p_hi = min(p_lo + per, pages);
+    const int* table = c.page_table + static_cast<long long>(slot) * c.max_pages + first;
+
+    // ---- q'
+    constexpr int ROWS = D / CL, TPR = SELECT_THREADS / ROWS, QUADS = D / 4 / TPR;      // rows of this CTA, threads per row, float4 per thread
+    const int row = rank * ROWS + tid / TPR, seg = tid % TPR;
+    float4 tr[QUADS];
+    const float4* T = reinterpret_cast<const float4*>(c.T_K_invT + (static_cast<long long>(h) * D + row) * D);
+#pragma unroll
+    for (int k = 0; k < QUADS; ++k) tr[k] = __ldg(T + seg + TPR * k);
+    if (warp < G) {
+        const uint2 w = *reinterpret_cast<const uint2*>(P.Q + (static_cast<long long>(b) * c.n_q + h * G + warp) * D + 4 * lane);
+        float x[4] = {bf16_bits_to_float(w.x & 0xffff), bf16_bits_to_float(w.x >> 16), bf16_bits_to_float(w.y & 0xffff), bf16_bits_to_float(w.y >> 16)};
+        if (P.pro.rope)
+            norm_rope_warp(x, lane, P.pro, h * G + warp, prologue_position(P.pro, S - 1, c.dev_status, lane == 0 && rank == 0));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sh.q[warp][4 * lane + e] = static_cast<double>(x[e]);
+    }
+    __syncthreads();
+    double acc[GP];
+#pragma unroll
+    for (int j = 0; j < GP; ++j) acc[j] = 0.0;
+#pragma unroll
+    for (int k = 0; k < QUADS; ++k) {
+        const double t0 = tr[k].x, t1 = tr[k].y, t2 = tr[k].z, t3 = tr[k].w;
+#pragma unroll
+        for (int j = 0; j < GP; ++j) {
+            if (j < G) {
+                const double2* q = reinterpret_cast<const double2*>(&sh.q[j][4 * (seg + TPR * k)]);
+                const double2 a = q[0], d = q[1];
+                acc[j] = fma(t0, a.x, fma(t1, a.y, fma(t2, d.x, fma(t3, d.y, acc[j]))));
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < GP; ++j)
+        if (j < G)
+#pragma unroll
+            for (int o = TPR / 2; o >= 1; o >>= 1) acc[j] += __shfl_xor_sync(FULL, acc[j], o);
+    if (CL > 1) asm volatile("barrier.cluster.wait;" ::: "memory");
+    if (seg < CL) {
+        double* q_of = CL > 1 ? cluster.map_shared_rank(&sh.qc[0][0], seg) : &sh.qc[0][0];
+#pragma unroll
+        for (int j = 0; j < GP; ++j) if (j < G) q_of[j * D + row] = acc[j];
+    }
+    for (int i = tid; i < SETS * 4 * 32; i += SELECT_THREADS) sh.frag[i] = make_uint4(0u, 0u, 0u, 0u);      // columns without a head
+    if (CL > 1) cluster.sync(); else __syncthreads();
+
+    // ---- the query as two signed bytes per channel: q' ~ (max|q'| / 32512) (256 hi + lo), in B fragments.  Row byte o of the
+    // bounds (lower 0 .. 127, upper 128 .. 255) is word (o % 16) / 4 of lane t = (o % 64) / 16 in group o / 64.
+    if (warp < G) {
+        double x[4], most = 0.0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { x[e] = sh.qc[warp][4 * lane + e]; most = fmax(most, fabs(x[e])); }
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) most = fmax(most, __shfl_xor_sync(FULL, most, o));
+        const bool usable = most > 0.0 && most < 3e38;          // otherwise all scores are 0: the lowest pages
+        const double per_unit = usable ? Q_MAX / most : 0.0;
+        unsigned word[2][2] = {{0u, 0u}, {0u, 0u}};             // [lower, upper][high, low digit]
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int v = usable ? min(max(__double2int_rn(x[e] * per_unit), -32512), 32512) : 0;
+            const int hi_digit = (v + 128) >> 8, lo_digit = v - 256 * hi_digit, side = v > 0 ? 1 : 0;
+            const unsigned wh = static_cast<unsigned>(hi_digit & 255) << (8 * e), wl = static_cast<unsigned>(lo_digit & 255) << (8 * e);
+            if (side) { word[1][0] |= wh; word[1][1] |= wl; } else { word[0][0] |= wh; word[0][1] |= wl; }
+        }
+        unsigned* frag = reinterpret_cast<unsigned*>(sh.frag);
+#pragma unroll
+        for (int side = 0; side < 2; ++side)
+#pragma unroll
+            for (int digit = 0; digit < 2; ++digit) {
+                const int set = MODE == 0 ? 0 : digit, column = MODE == 0 ? 2 * warp + digit : warp;
+                const int group = 2 * side + lane / 16, tl = (lane % 16) / 4;
+                frag[((set * 4 + group) * 32 + 4 * column + tl) * 4 + lane % 4] = word[side][digit];
+            }
+        if (lane == 0) sh.unit[warp] = usable ? static_cast<float>(__dmul_rn(most / Q_MAX, static_cast<double>(c.sm_scale))) : 0.f;
+    }
+    __syncthreads();
+
+    // ---- scores of this CTA's pages
+    uint4 bq[SETS][4];
+#pragma unroll
+    for (int k = 0; k < SETS * 4; ++k) bq[k / 4][k % 4] = sh.frag[k * 32 + lane];
+    constexpr int NH = MODE == 0 ? 1 : 2;                       // heads per lane: t, or 2 t and 2 t + 1
+    float unit[NH], best[NH];
+#pragma unroll
+    for (int k = 0; k < NH; ++k) { const int head = MODE == 0 ? t : 2 * t + k; unit[k] = head < G ? sh.unit[head] : 0.f; best[k] = -INFINITY; }
+    for (int p0 = p_lo + 16 * warp; p0 < p_hi; p0 += 16 * SELECT_WARPS) {
+        int page[2];
+        uint4 a[2][4];
+        int ex[2];
+#pragma unroll
+        for (int rs = 0; rs < 2; ++rs) {
+            const int p = p0 + g + 8 * rs;
+            page[rs] = p < p_hi ? __ldg(table + p) : -1;
+            const bool good = page[rs] >= 0 && page[rs] < c.n_pages;
+            if (!good) {
+                if (p < p_hi && t == 0) atomicOr(c.dev_status, WUSHKV_DEV_BAD_PAGE_ID);
+                page[rs] = -1;
+            }
+            const long long ph = static_cast<long long>(max(page[rs], 0)) * c.n_kv + h;
+            const uint4* src = reinterpret_cast<const uint4*>(P.bounds + ph * 2 * D) + t;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) a[rs][k] = __ldg(src + 4 * k);
+            ex[rs] = __ldg(P.exponents + ph);
+        }
+        int acc_i[SETS][4] = {};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int st = 0; st < SETS; ++st) {
+                mma_s8(acc_i[st], a[0][k].x, a[1][k].x, a[0][k].y, a[1][k].y, bq[st][k].x, bq[st][k].y);
+                mma_s8(acc_i[st], a[0][k].z, a[1][k].z, a[0][k].w, a[1][k].w, bq[st][k].z, bq[st][k].w);
+            }
+#pragma unroll
+        for (int rs = 0; rs < 2; ++rs) {
+            const int p = p0 + g + 8 * rs;
+            if (p >= p_hi) continue;
+            const float grid = __uint_as_float(static_cast<unsigned>(127 + ex[rs]) << 23);
+#pragma unroll
+            for (int k = 0; k < NH; ++k) {
+                const int head = MODE == 0 ? t : 2 * t + k;
+                if (head >= G) continue;
+                const int dot = MODE == 0 ? 256 * acc_i[0][2 * rs] + acc_i[0][2 * rs + 1] : 256 * acc_i[0][2 * rs + k] + acc_i[SETS - 1][2 * rs + k];
+                // one rounding to 32 bits, one of the product: an order that a plain computation can repeat
+                const float s = page[rs] >= 0 ? __fmul_rn(__int2float_rn(dot) * grid, unit[k]) : -INFINITY;
+                scores[head * per_max + p - p_lo] = s;
+                best[k] = fmaxf(best[k], s);
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < NH; ++k) {
+        best[k] = fmaxf(best[k], __shfl_xor_sync(FULL, best[k], 4));
+        best[k] = fmaxf(best[k], __shfl_xor_sync(FULL, best[k], 8));
+        best[k] = fmaxf(best[k], __shfl_xor_sync(FULL, best[k], 16));
+        const int head = MODE == 0 ? t : 2 * t + k;
+        if (g == 0) sh.warp_best[warp][head] = best[k];
+    }
+    __syncthreads();
+    if (tid < 8 * CL) {
+        const int head = tid & 7, peer = tid >> 3;
+        float m = -INFINITY;
+        if (head < G)
+#pragma unroll
+            for (int w = 0; w < SELECT_WARPS; ++w) m = fmaxf(m, sh.warp_best[w][head]);
+        float* to = CL > 1 ? cluster.map_shared_rank(&sh.best[0][0], peer) : &sh.best[0][0];
+        to[rank * 8 + head] = m;
+    }
+    if (CL > 1) cluster.sync(); else __syncthreads();
+
+    // ---- keys: bits of the distance below the best page (smaller is better)
+    unsigned* keys0 = CL > 1 ? cluster.map_shared_rank(keys, 0) : keys;
+    float top[GP];
+#pragma unroll
+    for (int j = 0; j < GP; ++j) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < CL; ++r) m = fmaxf(m, sh.best[r][j]);
+        top[j] = m == -INFINITY ? 0.f : m;
+    }
+    for (int p = p_lo + tid; p < p_hi; p += SELECT_THREADS) {
+        float key = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < GP; ++j) if (j < G) key = fmaxf(key, __fsub_rn(scores[j * per_max + p - p_lo], top[j]));
+        keys0[p] = __float_as_uint(key) & 0x7fffffffu;
+    }
+    if (CL > 1) cluster.sync(); else __syncthreads();
+    if (rank == 0) {
+        // ---- the n_select-th smallest: the largest v with fewer than n_select keys below it
+        unsigned kth = 0u;
+        for (int bit = 30; bit >= 0; --bit) {
+            const unsigned cand = kth | (1u << bit);
+            int n = 0;
+            for (int p = tid; p < pages; p += SELECT_THREADS) n += keys[p] < cand;
+            n = __reduce_add_sync(FULL, n);
+            if (lane == 0) sh.count[warp] = n;
+            __syncthreads();
+            int total = 0;
+#pragma unroll
+            for (int w = 0; w < SELECT_WARPS; ++w) total += sh.count[w];
+            if (total < P.n_select) kth = cand;
+            __syncthreads();
+        }
+        // ---- all below it, and of those equal to it the first ones; every thread lists a run of consecutive pages
+        const int run = (pages + SELECT_THREADS - 1) / SELECT_THREADS, r_lo = min(tid * run, pages), r_hi = min(r_lo + run, pages);
+        int below = 0, equal = 0;
+        for (int p = r_lo; p < r_hi; ++p) { below += keys[p] < kth; equal += keys[p] == kth; }
+        const auto prefix = [&](int x, int& total) {
+            int incl = x;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(FULL, incl, o);
+                if (lane >= o) incl += y;
+            }
+            __syncthreads();
+            if (lane == 31) sh.scan[warp] = incl;
+            __syncthreads();
+            int before = 0;
+            total = 0;
+#pragma unroll
+            for (int w = 0; w < SELECT_WARPS; ++w) { const int y = sh.scan[w]; if (w < warp) before += y; total += y; }
+            return before + incl - x;
+        };
+        int all_below, all_equal;
+        int below_before = prefix(below, all_below), equal_before = prefix(equal, all_equal);
+        const int room = P.n_select - all_below;          // places for keys equal to the n_select-th
+        for (int p = r_lo; p < r_hi; ++p) {
+            const unsigned k = keys[p];
+            if (k < kth) { out[below_before + min(equal_before, room)] = first + p; ++below_before; }
+            else if (k == kth) { if (equal_before < room) out[below_before + equal_before] = first + p; ++equal_before; }
+        }
+    }
+    if (P.early) pdl_wait();
+}
+
+template <int MODE, int CL>
+static int launch_select_cl(const SelectParams& P, cudaStream_t st) {
+    const auto kernel = select_pages_kernel<MODE, CL>;
+    const size_t smem = sizeof(SelectShared) + sizeof(float) * (static_cast<size_t>(P.c.G) * pages_per_cta(P.max_candidates, CL) + P.max_candidates);
+    if (!opt_in_dynamic_smem(reinterpret_cast<const void*>(kernel), 227 * 1024)) return WUSHKV_ECUDA;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = CL; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(CL, P.c.n_kv, P.batch);
+    cfg.blockDim = dim3(SELECT_THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, P) == cudaSuccess ? WUSHKV_OK : WUSHKV_ECUDA;
+}
+
+int launch_select(SelectParams P, int max_seq_len, cudaStream_t stream) {
+    const long long most = std::max<long long>(candidate_bound(P.c, max_seq_len), 1);
+    if (most > MAX_SELECT_PAGES) return WUSHKV_ECAPACITY;
+    P.max_candidates = static_cast<int>(most);
+    // CTAs per (sequence, KV head): enough for every SM to have one, but no fewer than 16 pages per warp
+    const long long clusters = static_cast<long long>(P.batch) * P.c.n_kv;
+    int cl = 1;
+    while (cl < 8 && clusters * cl < sm_count() && most > static_cast<long long>(cl) * 16 * SELECT_WARPS) cl *= 2;
+    // the scores and the keys have to fit in shared memory
+    const auto smem = [&](int k) { return sizeof(SelectShared) + sizeof(float) * (static_cast<size_t>(P.c.G) * pages_per_cta(P.max_candidates, k) + most); };
+    while (cl < 8 && smem(cl) > 227 * 1024) cl *= 2;
+    if (smem(cl) > 227 * 1024) return WUSHKV_ECAPACITY;
+    const bool mode0 = P.c.G <= 4;
+    switch (cl) {
+        case 1: return mode0 ? launch_select_cl<0, 1>(P, stream) : launch_select_cl<1, 1>(P, stream);
+        case 2: return mode0 ? launch_select_cl<0, 2>(P, stream) : launch_select_cl<1, 2>(P, stream);
+        case 4: return mode0 ? launch_select_cl<0, 4>(P, stream) : launch_select_cl<1, 4>(P, stream);
+        default: return mode0 ? launch_select_cl<0, 8>(P, stream) : launch_select_cl<1, 8>(P, stream);
+    }
+}
+
+}  // namespace wushkv
+
+using namespace wushkv;
+
+extern "C" int wushkv_update_page_bounds(const wushkv_cache* cache, int32_t batch, const int32_t* slot, const int32_t* seq_len, const int32_t* cu_new,
+                                         int32_t max_new, int8_t* bounds, int8_t* exponents, void* stream) {
+    BoundsParams P;
+    const int rc = make_view(cache, P.c);
+    if (rc != WUSHKV_OK) return rc;
+    if (batch <= 0 || batch > 65535 || max_new < 0 || !slot || !seq_len || !cu_new || !bounds || !exponents || !aligned(bounds, 16)) return WUSHKV_EINVAL;
+    if (max_new == 0) return WUSHKV_OK;
+    P.slot = slot; P.seq_len = seq_len; P.cu_new = cu_new; P.bounds = bounds; P.exponents = exponents;
+    const long long pages = (static_cast<long long>(max_new) + PAGE_TOKENS - 2) / PAGE_TOKENS + 1;       // that max_new consecutive tokens can touch
+    const dim3 grid(static_cast<unsigned>((pages * P.c.n_kv + 7) / 8), batch);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (P.c.bits == 2) page_bounds_kernel<2><<<grid, 256, 0, st>>>(P);
+    else if (P.c.bits == 3) page_bounds_kernel<3><<<grid, 256, 0, st>>>(P);
+    else page_bounds_kernel<4><<<grid, 256, 0, st>>>(P);
+    return cudaPeekAtLastError() == cudaSuccess ? WUSHKV_OK : WUSHKV_ECUDA;
+}
+
+extern "C" int wushkv_select_pages(const wushkv_cache* cache, int32_t batch, const int32_t* slot, const int32_t* seq_len, int32_t max_seq_len,
+                                   const uint16_t* Q, const wushkv_prologue* prologue, const int8_t* bounds, const int8_t* exponents,
+                                   int32_t n_select, int32_t* selected, void* stream) {
+    SelectParams P;
+    const int rc = make_view(cache, P.c);
+    if (rc != WUSHKV_OK) return rc;
+    if (batch <= 0 || batch > 65535 || P.c.n_kv > 65535 || max_seq_len <= 0 || n_select <= 0) return WUSHKV_EINVAL;
+    if (!slot || !seq_len || !Q || !bounds || !exponents || !selected || !aligned(Q, 16) || !aligned(bounds, 16)) return WUSHKV_EINVAL;
+    P.pro = Prologue{nullptr, 0, 0, nullptr, 0.f};
+    if (prologue && !make_prologue(prologue, prologue->q_norm_weight, P.pro)) return WUSHKV_EINVAL;
+    P.batch = batch; P.slot = slot; P.seq_len = seq_len; P.Q = Q;
+    P.bounds = reinterpret_cast<const signed char*>(bounds); P.exponents = reinterpret_cast<const signed char*>(exponents);
+    P.n_select = n_select; P.selected = selected; P.early = 0;
+    return launch_select(P, max_seq_len, static_cast<cudaStream_t>(stream));
+}
