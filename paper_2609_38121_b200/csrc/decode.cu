@@ -769,7 +769,7 @@ template <> struct OutputOf<false> { using type = float; static __device__ __for
 template <> struct OutputOf<true> { using type = unsigned short; static __device__ __forceinline__ unsigned short* of(const DecodeParams& P) { return P.O16; } };
 
 // SPARSE: the packed pages of a (sequence, KV head) are those of its list instead of all; the list is written by the selection
-// kernel ahead of this one, so nothing is staged before that has ended.  A warp has few units here (16 sequences x 8 heads x
+// kernel ahead of this one, so nothing is staged before that has ended (the work plan is made before, from the lengths alone).  A warp has few units here (16 sequences x 8 heads x
 // (64 pages + 17 window units) are 4.4 units for each of 2368 warps), so the two dependent loads list -> page table of a unit
 // would cost as much as the unit: the lanes make them for 32 units of a round at once.
 template <int BITS, int MODE, int STAGES, bool SPARSE>
@@ -801,7 +801,7 @@ __global__ void __launch_bounds__(main_warps(BITS, MODE) * 32, 1) decode_main_ke
     long long* plan_s = reinterpret_cast<long long*>(smem);
     static_assert((MAX_LOCAL_PLAN + 1) * sizeof(long long) <= static_cast<size_t>(MAIN_WARPS) * STAGES * REC, "the plan must fit in the staging area");
     const bool local_plan = P.batch <= MAX_LOCAL_PLAN;
-    if (P.q_early || !local_plan || SPARSE) pdl_wait();  // lengths from the append / plan from the preparation kernel / list from the selection kernel
+    if (P.q_early || !local_plan) pdl_wait();           // lengths from the append / plan from the preparation kernel
     for (int b = blockIdx.x * MAIN_WARPS * 32 + threadIdx.x; b < P.batch; b += gridDim.x * MAIN_WARPS * 32) {
         const int slot = __ldg(P.slot + b);
         if (slot < 0 || slot >= c.n_slots) atomicOr(c.dev_status, WUSHKV_DEV_BAD_SLOT);
@@ -910,6 +910,7 @@ __global__ void __launch_bounds__(main_warps(BITS, MODE) * 32, 1) decode_main_ke
         __syncwarp();
 
         // ================= producer: stages the units of this round, in order =====================
+        if (SPARSE) pdl_wait();                         // the list
         const long long round_L0 = L - round_units;      // flattened index of the round's first unit
         int p_seg = -1, p_u = 0, p_u1 = 0, p_qp = 0, p_head_off = 0, issued = 0;
         const int* p_ptab = nullptr;

@@ -48,8 +48,30 @@ __device__ __forceinline__ void halve(float* v, int lane, int bit) {
     }
 }
 
+// Two numbers per instruction, and minima and maxima of three.
+__device__ __forceinline__ unsigned long long pack2(float a, float b) {
+    unsigned long long d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ void unpack2(unsigned long long d, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(d)); }
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
+    unsigned long long d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ float min3(float a, float b, float c) { float d; asm("min.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
+__device__ __forceinline__ float max3(float a, float b, float c) { float d; asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
+
 // A warp per (page, head).  Lane (g, t) reads the code words of token rows g and g + 8 of every 16-token block, which hold the
 // channels 32 s + 16 hh + 8 u + 2 t + v of all s, hh, u, v: 32 running minima and maxima per lane, combined over g at the end.
+// What bounds it is instructions (256 codes per lane): a code becomes a float by a byte permute that puts its byte, masked to one
+// field, under the exponent of 2^23, the rest is done for the two token rows at once.
 template <int BITS>
 __global__ void __launch_bounds__(256) page_bounds_kernel(BoundsParams P) {
     constexpr int REC = record_bytes(BITS), CB = code_block_bytes(BITS);
@@ -76,6 +98,8 @@ __global__ void __launch_bounds__(256) page_bounds_kernel(BoundsParams P) {
         if (BITS == 3) high[bi] = __ldg(reinterpret_cast<const uint2*>(rec + k_hi_offset(3) + bi * 256) + lane);
         meta[bi] = __ldg(reinterpret_cast<const uint4*>(rec + meta_offset(BITS) + 128 * bi) + g);
     }
+    constexpr float MAGIC = 8388608.f;                       // 2^23
+    const unsigned long long unmagic = pack2(-MAGIC, -MAGIC);
     float lo[32], hi[32];
 #pragma unroll
     for (int j = 0; j < 32; ++j) { lo[j] = INFINITY; hi[j] = -INFINITY; }
@@ -92,25 +116,37 @@ __global__ void __launch_bounds__(256) page_bounds_kernel(BoundsParams P) {
             step[rs] = there ? f.x : 0.f;
             low[rs] = there ? f.y : NAN;                 // minimum and maximum pass over a NaN: a token that is not there, or a damaged one
         }
+        const unsigned long long low2 = pack2(low[0], low[1]);
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
+            // a code in bits F .. of its byte is code * 2^F; the step takes the 2^-F, both exact
+            constexpr unsigned FIELD = BITS == 4 ? 0x0F0F0F0Fu : 0x03030303u;
+            const int shift = BITS == 4 ? 4 * (s & 1) : 2 * s;
+            const float down = 1.f / static_cast<float>(1 << shift);
+            const unsigned long long step2 = pack2(step[0] * down, step[1] * down);
 #pragma unroll
             for (int hh = 0; hh < 2; ++hh) {
+                const uint4& q = words[bi][BITS == 4 ? s >> 1 : 0];
+                unsigned w[2] = {hh == 0 ? q.x : q.z, hh == 0 ? q.y : q.w};
+#pragma unroll
+                for (int rs = 0; rs < 2; ++rs) {
+                    w[rs] &= FIELD << shift;
+                    if (BITS == 3) {
+                        // the third bit, 4 * 2^F: for the uppermost field it would leave its byte, so that one is moved down
+                        const unsigned hb = ((rs == 0 ? high[bi].x : high[bi].y) >> (2 * s + hh)) & 0x01010101u;
+                        w[rs] = s < 3 ? w[rs] | (hb << (shift + 2)) : (w[rs] >> 2) | (hb << 6);
+                    }
+                }
+                const unsigned long long step_here = BITS == 3 && s == 3 ? pack2(step[0] * (1.f / 16.f), step[1] * (1.f / 16.f)) : step2;
 #pragma unroll
                 for (int by = 0; by < 4; ++by) {
-                    float v[2];
-#pragma unroll
-                    for (int rs = 0; rs < 2; ++rs) {
-                        const uint4& q = words[bi][BITS == 4 ? s >> 1 : 0];
-                        const unsigned w = hh == 0 ? (rs == 0 ? q.x : q.y) : (rs == 0 ? q.z : q.w);
-                        unsigned code = BITS == 4 ? (w >> (8 * by + 4 * (s & 1))) & 15u : (w >> (8 * by + 2 * s)) & 3u;
-                        if (BITS == 3) code |= (((rs == 0 ? high[bi].x : high[bi].y) >> (8 * by + 2 * s + hh)) & 1u) << 2;
-                        // step * code has at most 15 bits: the multiply-add rounds once, as the sum alone does
-                        v[rs] = fmaf(step[rs], static_cast<float>(code), low[rs]);
-                    }
+                    const float x0 = __uint_as_float(__byte_perm(w[0], 0x4B000000u, 0x7440u + by)), x1 = __uint_as_float(__byte_perm(w[1], 0x4B000000u, 0x7440u + by));
+                    // step * code has at most 15 bits: the multiply-add rounds once, as the sum alone does
+                    float v0, v1;
+                    unpack2(fma2(step_here, add2(pack2(x0, x1), unmagic), low2), v0, v1);
                     const int j = 8 * s + 4 * hh + by;
-                    lo[j] = fminf(lo[j], fminf(v[0], v[1]));
-                    hi[j] = fmaxf(hi[j], fmaxf(v[0], v[1]));
+                    lo[j] = min3(lo[j], v0, v1);
+                    hi[j] = max3(hi[j], v0, v1);
                 }
             }
         }
@@ -154,28 +190,96 @@ __device__ __forceinline__ void mma_s8(int (&c)[4], unsigned a0, unsigned a1, un
 }
 
 constexpr int SELECT_THREADS = 256, SELECT_WARPS = SELECT_THREADS / 32;
+constexpr int SELECT_BINS = 4 * SELECT_THREADS;
 
 // Shared memory of a CTA: fixed part, then the scores of its pages [heads][per], then (CTA 0) the keys of all pages.
 struct SelectShared {
     double q[8][D];                   // the queries, in 64 bits
     double qc[8][D];                  // q' of all CTAs' rows
     uint4 frag[2 * 4 * 32];           // B fragments: [digit set][64 bytes of bounds][lane]
+    uint4 bins[SELECT_THREADS];       // CTA 0: pages per bin of the range of keys
     float unit[8];                    // score of one unit of 2^e dot
     float warp_best[SELECT_WARPS][8];
-    float best[16][8];                // per CTA of the cluster: largest score of its pages, per head
-    int count[SELECT_WARPS];
+    float best[8][8];                 // per CTA of the cluster: largest score of its pages, per head
     int scan[SELECT_WARPS];
+    unsigned most;                    // CTA 0: largest finite key
+    int bin, before, inside;          // CTA 0: the bin of the n_select-th key, keys in the bins ahead, keys in it
+    unsigned kth;
+    int n_list;
+    unsigned list[SELECT_THREADS];    // keys of that bin
 };
 
 __host__ __device__ inline int pages_per_cta(int pages, int cl) { return ((pages + cl - 1) / cl + 15) / 16 * 16; }
+
+// Loads that stay where they are written: ahead of the work that their latency is to hide behind.
+__device__ __forceinline__ uint4 ld_early(const uint4* p) {
+    uint4 v;
+    asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ int ld_early_s8(const signed char* p) {
+    int v;
+    asm volatile("ld.global.nc.s8 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
+
+// Sums NV numbers per lane over groups of LANES lanes.  While there are several, each step hands half of them to the other side;
+// afterwards lane l of the group holds the totals of FIRST(l) .. FIRST(l) + LEFT - 1, and REPLICAS lanes hold the same.
+template <int NV, int LANES>
+struct GroupSum {
+    static constexpr int LEFT = NV > LANES ? NV / LANES : 1, REPLICAS = LANES > NV ? LANES / NV : 1;
+    template <int N, int O>
+    static __device__ __forceinline__ void step(double* v, int l) {
+        if constexpr (O >= 1) {
+            if constexpr (N > 1) {
+                const bool upper = (l & O) != 0;
+#pragma unroll
+                for (int i = 0; i < N / 2; ++i) {
+                    const double send = upper ? v[i] : v[i + N / 2], keep = upper ? v[i + N / 2] : v[i];
+                    v[i] = keep + __shfl_xor_sync(FULL, send, O);
+                }
+                step<N / 2, O / 2>(v, l);
+            } else {
+                v[0] += __shfl_xor_sync(FULL, v[0], O);
+                step<1, O / 2>(v, l);
+            }
+        }
+    }
+    static __device__ __forceinline__ void sum(double* v, int l) { step<NV, LANES / 2>(v, l); }
+    static __device__ __forceinline__ int first(int l) { return l / REPLICAS * LEFT; }
+    static __device__ __forceinline__ int replica(int l) { return l % REPLICAS; }
+};
+
+// One tile of 16 pages as a lane reads it: 64 bytes of the bounds of rows g and g + 8 and the rows' exponents.
+struct BoundsTile {
+    uint4 a[2][4];
+    int ex[2];
+    bool good[2];
+    __device__ __forceinline__ void load(const SelectParams& P, const int* table, int h, int p0, int p_hi, int g, int t) {
+#pragma unroll
+        for (int rs = 0; rs < 2; ++rs) {
+            const int p = p0 + g + 8 * rs;
+            const int page = p < p_hi ? __ldg(table + p) : -1;
+            good[rs] = page >= 0 && page < P.c.n_pages;
+            if (p < p_hi && !good[rs] && t == 0) atomicOr(P.c.dev_status, WUSHKV_DEV_BAD_PAGE_ID);
+            const long long ph = static_cast<long long>(good[rs] ? page : 0) * P.c.n_kv + h;
+            const uint4* src = reinterpret_cast<const uint4*>(P.bounds + ph * 2 * D) + t;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) a[rs][k] = ld_early(src + 4 * k);
+            ex[rs] = ld_early_s8(P.exponents + ph);
+        }
+    }
+};
 
 // One cluster of CL CTAs per (sequence, KV head).
 //   1. q' = T_K^{-T} q: each CTA forms 128 / CL rows of it and hands them to the others through distributed shared memory.
 //   2. Each CTA scores its share of the pages, 16 pages per warp and step: bounds straight from global memory into the A
 //      fragments (their bytes are consecutive in k, so that one 16-byte load per lane and row is two registers of two k-steps).
+//      The first step's loads are in flight during 1, the next step's during each step.
 //   3. The largest score per head of all CTAs, the key of every page (how far it is below the best page of the head that it
 //      matters most to), sent to CTA 0.
-//   4. CTA 0 finds the n_select-th largest key bit by bit and lists the pages.
+//   4. CTA 0 counts the keys in bins of equal width, finds the bin of the n_select-th smallest and its rank there by comparing
+//      the bin's few keys with each other, and lists the pages.
 // All of it is latency: the bounds of 16 sequences x 8 heads x 510 pages are 17 MB, 2.6 us at the copy rate.
 template <int MODE, int CL>
 __global__ void __launch_bounds__(SELECT_THREADS) select_pages_kernel(SelectParams P) {
@@ -188,7 +292,9 @@ __global__ void __launch_bounds__(SELECT_THREADS) select_pages_kernel(SelectPara
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3, G = c.G;
     if (!P.early) pdl_wait();
     pdl_launch_dependents();
-    if (CL > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");       // the other CTAs' shared memory exists once they have arrived
+    // nobody writes into another CTA's shared memory before that CTA has come here and zeroed what the others add to
+    if (tid == 0) { sh.most = 0u; sh.n_list = 0; }
+    if (CL > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
 
     // ---- candidates
     const int S = __ldcg(P.seq_len + b), slot = P.slot[b];
@@ -213,7 +319,7 @@ __global__ void __launch_bounds__(SELECT_THREADS) select_pages_kernel(SelectPara
     if (all) {
         if (rank == 0)
             for (int i = tid; i < P.n_select; i += SELECT_THREADS) out[i] = i < pages ? first + i : -1;
-        if (CL > 1) asm volatile("barrier.cluster.wait;" ::: "memory");
+        if (CL > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
         if (P.early) pdl_wait();
         return;
     }
@@ -223,49 +329,62 @@ __global__ void __launch_bounds__(SELECT_THREADS) select_pages_kernel(SelectPara
     const int per = pages_per_cta(pages, CL), p_lo = min(rank * per, pages), p_hi = min(p_lo + per, pages);
     const int* table = c.page_table + static_cast<long long>(slot) * c.max_pages + first;
 
-    // ---- q'
-    constexpr int ROWS = D / CL, TPR = SELECT_THREADS / ROWS, QUADS = D / 4 / TPR;      // rows of this CTA, threads per row, float4 per thread
-    const int row = rank * ROWS + tid / TPR, seg = tid % TPR;
-    float4 tr[QUADS];
-    const float4* T = reinterpret_cast<const float4*>(c.T_K_invT + (static_cast<long long>(h) * D + row) * D);
+    // ---- q', two rows per thread (a query element read from shared memory serves both)
+    constexpr int ROWS = D / CL, PAIRS = ROWS / 2, TPP = SELECT_THREADS / PAIRS, QUADS = D / 4 / TPP;      // threads per pair of rows, float4 per thread and row
+    const int row = rank * ROWS + tid / TPP, seg = tid % TPP;
+    const uint4* T = reinterpret_cast<const uint4*>(c.T_K_invT + (static_cast<long long>(h) * D + row) * D);
+    uint4 tr[2][QUADS];
 #pragma unroll
-    for (int k = 0; k < QUADS; ++k) tr[k] = __ldg(T + seg + TPR * k);
-    if (warp < G) {
-        const uint2 w = *reinterpret_cast<const uint2*>(P.Q + (static_cast<long long>(b) * c.n_q + h * G + warp) * D + 4 * lane);
-        float x[4] = {bf16_bits_to_float(w.x & 0xffff), bf16_bits_to_float(w.x >> 16), bf16_bits_to_float(w.y & 0xffff), bf16_bits_to_float(w.y >> 16)};
-        if (P.pro.rope)
-            norm_rope_warp(x, lane, P.pro, h * G + warp, prologue_position(P.pro, S - 1, c.dev_status, lane == 0 && rank == 0));
+    for (int k = 0; k < QUADS; ++k) { tr[0][k] = ld_early(T + seg + TPP * k); tr[1][k] = ld_early(T + PAIRS * (D / 4) + seg + TPP * k); }
+    BoundsTile tile;
+    tile.load(P, table, h, p_lo + 16 * warp, p_hi, g, t);
+    if (warp < GP) {
+        float x[4] = {0.f, 0.f, 0.f, 0.f};              // slots without a head are zero
+        if (warp < G) {
+            const uint2 w = *reinterpret_cast<const uint2*>(P.Q + (static_cast<long long>(b) * c.n_q + h * G + warp) * D + 4 * lane);
+            x[0] = bf16_bits_to_float(w.x & 0xffff); x[1] = bf16_bits_to_float(w.x >> 16);
+            x[2] = bf16_bits_to_float(w.y & 0xffff); x[3] = bf16_bits_to_float(w.y >> 16);
+            if (P.pro.rope)
+                norm_rope_warp(x, lane, P.pro, h * G + warp, prologue_position(P.pro, S - 1, c.dev_status, lane == 0 && rank == 0));
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) sh.q[warp][4 * lane + e] = static_cast<double>(x[e]);
     }
+    sh.bins[tid] = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = tid; i < SETS * 4 * 32; i += SELECT_THREADS) sh.frag[i] = make_uint4(0u, 0u, 0u, 0u);      // columns without a head
     __syncthreads();
-    double acc[GP];
+    double acc[2 * GP];                                 // [row][head]
 #pragma unroll
-    for (int j = 0; j < GP; ++j) acc[j] = 0.0;
+    for (int j = 0; j < 2 * GP; ++j) acc[j] = 0.0;
 #pragma unroll
     for (int k = 0; k < QUADS; ++k) {
-        const double t0 = tr[k].x, t1 = tr[k].y, t2 = tr[k].z, t3 = tr[k].w;
+        double tv[2][4];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            tv[r][0] = __uint_as_float(tr[r][k].x); tv[r][1] = __uint_as_float(tr[r][k].y);
+            tv[r][2] = __uint_as_float(tr[r][k].z); tv[r][3] = __uint_as_float(tr[r][k].w);
+        }
 #pragma unroll
         for (int j = 0; j < GP; ++j) {
-            if (j < G) {
-                const double2* q = reinterpret_cast<const double2*>(&sh.q[j][4 * (seg + TPR * k)]);
-                const double2 a = q[0], d = q[1];
-                acc[j] = fma(t0, a.x, fma(t1, a.y, fma(t2, d.x, fma(t3, d.y, acc[j]))));
-            }
+            const double2* q = reinterpret_cast<const double2*>(&sh.q[j][4 * (seg + TPP * k)]);
+            const double2 lo = q[0], hi = q[1];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) acc[r * GP + j] = fma(tv[r][0], lo.x, fma(tv[r][1], lo.y, fma(tv[r][2], hi.x, fma(tv[r][3], hi.y, acc[r * GP + j]))));
         }
     }
+    using Sum = GroupSum<2 * GP, TPP>;
+    Sum::sum(acc, seg);
+    if (CL > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
 #pragma unroll
-    for (int j = 0; j < GP; ++j)
-        if (j < G)
+    for (int peer = 0; peer < CL; ++peer) {
+        if (peer % Sum::REPLICAS != Sum::replica(seg)) continue;
+        double* q_of = CL > 1 ? cluster.map_shared_rank(&sh.qc[0][0], peer) : &sh.qc[0][0];
 #pragma unroll
-            for (int o = TPR / 2; o >= 1; o >>= 1) acc[j] += __shfl_xor_sync(FULL, acc[j], o);
-    if (CL > 1) asm volatile("barrier.cluster.wait;" ::: "memory");
-    if (seg < CL) {
-        double* q_of = CL > 1 ? cluster.map_shared_rank(&sh.qc[0][0], seg) : &sh.qc[0][0];
-#pragma unroll
-        for (int j = 0; j < GP; ++j) if (j < G) q_of[j * D + row] = acc[j];
+        for (int i = 0; i < Sum::LEFT; ++i) {
+            const int k = Sum::first(seg) + i;
+            q_of[(k % GP) * D + row + (k / GP) * PAIRS] = acc[i];
+        }
     }
-    for (int i = tid; i < SETS * 4 * 32; i += SELECT_THREADS) sh.frag[i] = make_uint4(0u, 0u, 0u, 0u);      // columns without a head
     if (CL > 1) cluster.sync(); else __syncthreads();
 
     // ---- the query as two signed bytes per channel: q' ~ (max|q'| / 32512) (256 hi + lo), in B fragments.  Row byte o of the
@@ -282,9 +401,9 @@ __global__ void __launch_bounds__(SELECT_THREADS) select_pages_kernel(SelectPara
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int v = usable ? min(max(__double2int_rn(x[e] * per_unit), -32512), 32512) : 0;
-            const int hi_digit = (v + 128) >> 8, lo_digit = v - 256 * hi_digit, side = v > 0 ? 1 : 0;
+            const int hi_digit = (v + 128) >> 8, lo_digit = v - 256 * hi_digit;
             const unsigned wh = static_cast<unsigned>(hi_digit & 255) << (8 * e), wl = static_cast<unsigned>(lo_digit & 255) << (8 * e);
-            if (side) { word[1][0] |= wh; word[1][1] |= wl; } else { word[0][0] |= wh; word[0][1] |= wl; }
+            if (v > 0) { word[1][0] |= wh; word[1][1] |= wl; } else { word[0][0] |= wh; word[0][1] |= wl; }
         }
         unsigned* frag = reinterpret_cast<unsigned*>(sh.frag);
 #pragma unroll
@@ -308,44 +427,28 @@ __global__ void __launch_bounds__(SELECT_THREADS) select_pages_kernel(SelectPara
 #pragma unroll
     for (int k = 0; k < NH; ++k) { const int head = MODE == 0 ? t : 2 * t + k; unit[k] = head < G ? sh.unit[head] : 0.f; best[k] = -INFINITY; }
     for (int p0 = p_lo + 16 * warp; p0 < p_hi; p0 += 16 * SELECT_WARPS) {
-        int page[2];
-        uint4 a[2][4];
-        int ex[2];
-#pragma unroll
-        for (int rs = 0; rs < 2; ++rs) {
-            const int p = p0 + g + 8 * rs;
-            page[rs] = p < p_hi ? __ldg(table + p) : -1;
-            const bool good = page[rs] >= 0 && page[rs] < c.n_pages;
-            if (!good) {
-                if (p < p_hi && t == 0) atomicOr(c.dev_status, WUSHKV_DEV_BAD_PAGE_ID);
-                page[rs] = -1;
-            }
-            const long long ph = static_cast<long long>(max(page[rs], 0)) * c.n_kv + h;
-            const uint4* src = reinterpret_cast<const uint4*>(P.bounds + ph * 2 * D) + t;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) a[rs][k] = __ldg(src + 4 * k);
-            ex[rs] = __ldg(P.exponents + ph);
-        }
+        const BoundsTile now = tile;
+        if (p0 + 16 * SELECT_WARPS < p_hi) tile.load(P, table, h, p0 + 16 * SELECT_WARPS, p_hi, g, t);
         int acc_i[SETS][4] = {};
 #pragma unroll
         for (int k = 0; k < 4; ++k)
 #pragma unroll
             for (int st = 0; st < SETS; ++st) {
-                mma_s8(acc_i[st], a[0][k].x, a[1][k].x, a[0][k].y, a[1][k].y, bq[st][k].x, bq[st][k].y);
-                mma_s8(acc_i[st], a[0][k].z, a[1][k].z, a[0][k].w, a[1][k].w, bq[st][k].z, bq[st][k].w);
+                mma_s8(acc_i[st], now.a[0][k].x, now.a[1][k].x, now.a[0][k].y, now.a[1][k].y, bq[st][k].x, bq[st][k].y);
+                mma_s8(acc_i[st], now.a[0][k].z, now.a[1][k].z, now.a[0][k].w, now.a[1][k].w, bq[st][k].z, bq[st][k].w);
             }
 #pragma unroll
         for (int rs = 0; rs < 2; ++rs) {
             const int p = p0 + g + 8 * rs;
             if (p >= p_hi) continue;
-            const float grid = __uint_as_float(static_cast<unsigned>(127 + ex[rs]) << 23);
+            const float grid = __uint_as_float(static_cast<unsigned>(127 + now.ex[rs]) << 23);
 #pragma unroll
             for (int k = 0; k < NH; ++k) {
                 const int head = MODE == 0 ? t : 2 * t + k;
                 if (head >= G) continue;
                 const int dot = MODE == 0 ? 256 * acc_i[0][2 * rs] + acc_i[0][2 * rs + 1] : 256 * acc_i[0][2 * rs + k] + acc_i[SETS - 1][2 * rs + k];
                 // one rounding to 32 bits, one of the product: an order that a plain computation can repeat
-                const float s = page[rs] >= 0 ? __fmul_rn(__int2float_rn(dot) * grid, unit[k]) : -INFINITY;
+                const float s = now.good[rs] ? __fmul_rn(__int2float_rn(dot) * grid, unit[k]) : -INFINITY;
                 scores[head * per_max + p - p_lo] = s;
                 best[k] = fmaxf(best[k], s);
             }
@@ -381,51 +484,94 @@ __global__ void __launch_bounds__(SELECT_THREADS) select_pages_kernel(SelectPara
         for (int r = 0; r < CL; ++r) m = fmaxf(m, sh.best[r][j]);
         top[j] = m == -INFINITY ? 0.f : m;
     }
+    constexpr unsigned INF_BITS = 0x7f800000u;
+    unsigned most = 0u;
     for (int p = p_lo + tid; p < p_hi; p += SELECT_THREADS) {
         float key = -INFINITY;
 #pragma unroll
         for (int j = 0; j < GP; ++j) if (j < G) key = fmaxf(key, __fsub_rn(scores[j * per_max + p - p_lo], top[j]));
-        keys0[p] = __float_as_uint(key) & 0x7fffffffu;
+        const unsigned u = __float_as_uint(key) & 0x7fffffffu;
+        keys0[p] = u;
+        if (u < INF_BITS) most = max(most, u);
     }
+    most = __reduce_max_sync(FULL, most);
+    if (lane == 0 && most > 0u) atomicMax(CL > 1 ? cluster.map_shared_rank(&sh.most, 0) : &sh.most, most);
     if (CL > 1) cluster.sync(); else __syncthreads();
     if (rank == 0) {
-        // ---- the n_select-th smallest: the largest v with fewer than n_select keys below it
-        unsigned kth = 0u;
-        for (int bit = 30; bit >= 0; --bit) {
-            const unsigned cand = kth | (1u << bit);
-            int n = 0;
-            for (int p = tid; p < pages; p += SELECT_THREADS) n += keys[p] < cand;
-            n = __reduce_add_sync(FULL, n);
-            if (lane == 0) sh.count[warp] = n;
-            __syncthreads();
-            int total = 0;
-#pragma unroll
-            for (int w = 0; w < SELECT_WARPS; ++w) total += sh.count[w];
-            if (total < P.n_select) kth = cand;
-            __syncthreads();
-        }
-        // ---- all below it, and of those equal to it the first ones; every thread lists a run of consecutive pages
-        const int run = (pages + SELECT_THREADS - 1) / SELECT_THREADS, r_lo = min(tid * run, pages), r_hi = min(r_lo + run, pages);
-        int below = 0, equal = 0;
-        for (int p = r_lo; p < r_hi; ++p) { below += keys[p] < kth; equal += keys[p] == kth; }
-        const auto prefix = [&](int x, int& total) {
+        // ---- bins of equal width from 0 to the largest key; the product is monotonic in the key, so bins are in the keys' order
+        const float width = __uint_as_float(sh.most), per_bin = width > 0.f ? (SELECT_BINS - 1) / width : 0.f;
+        const auto bin_of = [&](unsigned u) {
+            return u < INF_BITS ? min(static_cast<int>(__uint_as_float(u) * per_bin), SELECT_BINS - 1) : SELECT_BINS - 1;
+        };
+        unsigned* bins = reinterpret_cast<unsigned*>(sh.bins);
+        for (int p = tid; p < pages; p += SELECT_THREADS) atomicAdd(bins + bin_of(keys[p]), 1u);
+        const auto prefix = [&](int x) {                        // exclusive prefix sum over the CTA
             int incl = x;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const int y = __shfl_up_sync(FULL, incl, o);
                 if (lane >= o) incl += y;
             }
-            __syncthreads();
             if (lane == 31) sh.scan[warp] = incl;
             __syncthreads();
             int before = 0;
-            total = 0;
 #pragma unroll
-            for (int w = 0; w < SELECT_WARPS; ++w) { const int y = sh.scan[w]; if (w < warp) before += y; total += y; }
+            for (int w = 0; w < SELECT_WARPS; ++w) before += w < warp ? sh.scan[w] : 0;
             return before + incl - x;
         };
-        int all_below, all_equal;
-        int below_before = prefix(below, all_below), equal_before = prefix(equal, all_equal);
+        __syncthreads();
+        const uint4 mine = sh.bins[tid];
+        const int counts[4] = {static_cast<int>(mine.x), static_cast<int>(mine.y), static_cast<int>(mine.z), static_cast<int>(mine.w)};
+        int before = prefix(counts[0] + counts[1] + counts[2] + counts[3]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (before < P.n_select && P.n_select <= before + counts[e]) { sh.bin = 4 * tid + e; sh.before = before; sh.inside = counts[e]; }
+            before += counts[e];
+        }
+        __syncthreads();
+        const int bin = sh.bin, inside = sh.inside, wanted = P.n_select - sh.before - 1;      // rank of the n_select-th key in its bin
+        unsigned kth = 0u;
+        if (inside <= SELECT_THREADS) {
+            for (int p = tid; p < pages; p += SELECT_THREADS) {
+                const unsigned u = keys[p];
+                if (bin_of(u) == bin) sh.list[atomicAdd(&sh.n_list, 1)] = u;
+            }
+            __syncthreads();
+            if (tid < inside) {
+                const unsigned u = sh.list[tid];
+                int less = 0, same = 0;
+                for (int k = 0; k < inside; ++k) { less += sh.list[k] < u; same += sh.list[k] == u; }
+                if (less <= wanted && wanted < less + same) sh.kth = u;      // equal keys write the same
+            }
+            __syncthreads();
+            kth = sh.kth;
+        } else {
+            // many keys that are (almost) the same: bit by bit, the largest v with fewer than n_select keys below it
+            for (int bit = 30; bit >= 0; --bit) {
+                const unsigned cand = kth | (1u << bit);
+                int n = 0;
+                for (int p = tid; p < pages; p += SELECT_THREADS) n += keys[p] < cand;
+                n = __reduce_add_sync(FULL, n);
+                __syncthreads();
+                if (lane == 0) sh.scan[warp] = n;
+                __syncthreads();
+                int total = 0;
+#pragma unroll
+                for (int w = 0; w < SELECT_WARPS; ++w) total += sh.scan[w];
+                if (total < P.n_select) kth = cand;
+            }
+        }
+        __syncthreads();                                        // the readers of sh.scan
+        // ---- all below it, and of those equal to it the first ones; every thread lists a run of consecutive pages
+        const int run = (pages + SELECT_THREADS - 1) / SELECT_THREADS, r_lo = min(tid * run, pages), r_hi = min(r_lo + run, pages);
+        int below = 0, equal = 0;
+        for (int p = r_lo; p < r_hi; ++p) { below += keys[p] < kth; equal += keys[p] == kth; }
+        static_assert(MAX_SELECT_PAGES < (1 << 15), "two counts in one prefix sum");
+        const int packed = prefix((below << 16) + equal);
+        int all_below = 0;
+#pragma unroll
+        for (int w = 0; w < SELECT_WARPS; ++w) all_below += sh.scan[w] >> 16;
+        int below_before = packed >> 16, equal_before = packed & 0xffff;
         const int room = P.n_select - all_below;          // places for keys equal to the n_select-th
         for (int p = r_lo; p < r_hi; ++p) {
             const unsigned k = keys[p];
@@ -462,8 +608,9 @@ int launch_select(SelectParams P, int max_seq_len, cudaStream_t stream) {
     P.max_candidates = static_cast<int>(most);
     // CTAs per (sequence, KV head): enough for every SM to have one, but no fewer than 16 pages per warp
     const long long clusters = static_cast<long long>(P.batch) * P.c.n_kv;
-    int cl = 1;
-    while (cl < 8 && clusters * cl < sm_count() && most > static_cast<long long>(cl) * 16 * SELECT_WARPS) cl *= 2;
+    int cl = knobs().select_cluster;
+    if (cl != 2 && cl != 4 && cl != 8) cl = 1;
+    while (knobs().select_cluster == 0 && cl < 8 && clusters * cl < sm_count() && most > static_cast<long long>(cl) * 16 * SELECT_WARPS) cl *= 2;
     // the scores and the keys have to fit in shared memory
     const auto smem = [&](int k) { return sizeof(SelectShared) + sizeof(float) * (static_cast<size_t>(P.c.G) * pages_per_cta(P.max_candidates, k) + most); };
     while (cl < 8 && smem(cl) > 227 * 1024) cl *= 2;

@@ -194,6 +194,27 @@ def test_a_long_sequence_on_one_head_uses_a_cluster():
     s.check(40)
 
 
+@pytest.mark.parametrize("n_q,n_kv", [(3, 1), (8, 1)])
+def test_every_cluster_size_selects_the_same(n_q, n_kv):
+    s = Sparse([40000, 9000, 3000], n_q, n_kv, 2, seed=22)
+    q, Q = s.queries()
+    ref = s.oracle_select(q, 624)
+    for n_select in (1, 40, 150, 300, 624):
+        want = ref if n_select == 624 else s.oracle_select(q, n_select)
+        for cluster in (1, 2, 4, 8, 0):
+            s.B.set_test_option("select_cluster", cluster)
+            try:
+                sel = s.torch.full((3, n_kv, n_select), -9, dtype=s.torch.int32, device="cuda")
+                s.B.select_pages(s.L.cache.desc, 3, s.L.slot, s.L.seq_len, s.L.max_seq_len, Q, s.bounds, s.exponents, n_select, sel)
+                assert np.array_equal(sel.cpu().numpy(), want), (n_select, cluster)
+                # more pages with the same key than a bin's list holds
+                s.B.select_pages(s.L.cache.desc, 3, s.L.slot, s.L.seq_len, s.L.max_seq_len, s.torch.zeros_like(Q), s.bounds, s.exponents, n_select, sel)
+                pages = np.array([S.packed_range(n, 4, 64, 1)[3] for n in s.L.done])
+                assert np.array_equal(sel.cpu().numpy()[:, 0], np.where(np.arange(n_select)[None] < np.minimum(pages, n_select)[:, None], np.arange(n_select)[None], -1))
+            finally:
+                s.B.set_test_option("select_cluster", 0)
+
+
 def test_equal_keys_go_to_the_lower_page():
     s = Sparse([3000, 3000], 8, 2, 2, seed=13)
     s.bounds[:] = s.bounds[:1]
