@@ -60,7 +60,6 @@ constexpr float MAX_SLACK = 3.f;
 // limit it) instead of several CTAs of 4: the hardware warp scheduler serves the warps of an older CTA first, so with
 // several CTAs per SM equal slices finished up to 15 us apart.
 __host__ __device__ constexpr int main_warps(int bits, int mode) { return (bits == 2 && mode == 0) ? 16 : 12; }
-constexpr int WIN_TOKENS = 8;             // window tokens per work unit
 constexpr int WIN_ROW = 272;              // padded bytes per staged bf16 row (conflict-free ldmatrix)
 constexpr int WIN_V_OFF = WIN_TOKENS * WIN_ROW;
 
@@ -88,10 +87,6 @@ struct DecodeParams {
     unsigned short* O16; // sparse attention: the outputs as bf16 (O is not used)
 };
 
-// Arrival counters of a (sequence, KV head)'s 8 query head slots for the main kernel's merge, zeroed by the preparation kernel:
-// in the unused half of the head's integer fragments.
-__device__ __forceinline__ int* arrival_counters(const DecodeParams& P, long long bh) { return reinterpret_cast<int*>(P.qfrag + bh * 256 + 128); }
-
 // shift of the code field used by k-step / channel block idx (0..7) inside its 16-bit lane, after
 // the optional whole-word shift: the fp16 value of the masked field is code * 2^(field_shift - 24)
 template <int BITS>
@@ -101,40 +96,6 @@ __host__ __device__ constexpr int field_shift(int idx) {
 // bf16x2 bit pattern of (2^e, 2^e)
 __host__ __device__ constexpr unsigned bf16x2_pow2(int e) {
     return (static_cast<unsigned>(e + 127) << 7) | (static_cast<unsigned>(e + 127) << 23);
-}
-
-// How one sequence decomposes into work units (identical for all of its KV heads).
-struct SeqInfo {
-    int slot;
-    int q_lo, q_hi;          // positions read from the packed codes: [q_lo, q_hi)
-    int first_page, qp;      // packed pages covering them
-    int n_sink, recent_lo;   // window tokens: positions [0, n_sink) and [recent_lo, S)
-    int n_win;               // window tokens
-    int U;                   // qp + ceil(n_win / WIN_TOKENS)
-};
-
-__device__ __forceinline__ SeqInfo seq_info(const CacheView& c, int S, int slot) {
-    SeqInfo si;
-    si.slot = slot;
-    if (S <= 0 || slot < 0 || slot >= c.n_slots) {
-        si.q_lo = si.q_hi = 0; si.first_page = si.qp = 0; si.n_sink = si.recent_lo = si.n_win = si.U = 0;
-        return si;
-    }
-    const int nq = n_quantized(S - c.lag, c.s_sink, c.s_keep, c.s_flush);
-    si.q_lo = c.s_sink; si.q_hi = c.s_sink + nq;
-    si.first_page = si.q_lo / PAGE_TOKENS;
-    si.qp = nq > 0 ? (si.q_hi - 1) / PAGE_TOKENS - si.first_page + 1 : 0;
-    si.n_sink = min(S, c.s_sink);
-    si.recent_lo = c.s_sink + nq;
-    si.n_win = si.n_sink + max(0, S - si.recent_lo);
-    si.U = si.qp + (si.n_win + WIN_TOKENS - 1) / WIN_TOKENS;
-    return si;
-}
-
-// Sparse attention reads at most n_select of the packed pages, the first min(n_select, qp) entries of the (sequence, KV head)'s list.
-__device__ __forceinline__ SeqInfo sparse_info(SeqInfo si, int n_select) {
-    if (si.qp > n_select) { si.U -= si.qp - n_select; si.qp = n_select; }
-    return si;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -156,7 +117,6 @@ __global__ void __launch_bounds__(PREP_THREADS) decode_prep_kernel(DecodeParams 
     __shared__ float qp_s[8][D];
     __shared__ float red_abs[8][4];
     __shared__ int red_isum[8][4];
-    __shared__ long long scan_s[4];
     float (*q_s)[D] = reinterpret_cast<float (*)[D]>(buf);
     const int h = blockIdx.x, b = blockIdx.y, G = P.c.G;
     const int i = threadIdx.x, lane = i & 31, warp = i >> 5;
@@ -214,34 +174,13 @@ __global__ void __launch_bounds__(PREP_THREADS) decode_prep_kernel(DecodeParams 
     }
     if (P.batch > MAX_LOCAL_PLAN && first_cta) {       // work plan for the main kernel: exclusive prefix of units per sequence
         if (P.q_early) pdl_wait();                      // the lengths come from the append
-        long long carry = 0;
-        for (int base = 0; base < P.batch; base += 128) {
-            const int bb = base + i;
-            long long u = 0;
-            if (i < 128 && bb < P.batch) {
-                const SeqInfo si = seq_info(P.c, __ldcg(P.seq_len + bb), __ldg(P.slot + bb));
-                u = P.n_select > 0 ? sparse_info(si, P.n_select).U : si.U;
-            }
-            long long incl = u;
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long v = __shfl_up_sync(FULL, incl, o);
-                if (lane >= o) incl += v;
-            }
-            if (lane == 31 && warp < 4) scan_s[warp] = incl;
-            __syncthreads();
-            long long before = 0;
-            for (int w = 0; w < warp && w < 4; ++w) before += scan_s[w];
-            if (i < 128 && bb < P.batch) P.plan[bb + 1] = carry + before + incl;
-            carry += scan_s[0] + scan_s[1] + scan_s[2] + scan_s[3];
-            __syncthreads();
-        }
-        if (i == 0) P.plan[0] = 0;
+        write_plan(P.c, P.batch, P.seq_len, P.slot, P.n_select, P.plan);
     }
     __syncthreads();
     if (i >= D) return;                    // the fragment stage has one thread per channel
     const int ch = i;
     const long long bh = static_cast<long long>(b) * P.c.n_kv + h;
-    if (ch < 8) arrival_counters(P, bh)[ch] = 0;
+    if (ch < 8) arrival_counters(P.qfrag, bh)[ch] = 0;
     float acc[GP];
 #pragma unroll
     for (int g = 0; g < GP; ++g) acc[g] = g < G ? qp_s[g][ch] : 0.f;
@@ -724,7 +663,7 @@ __device__ __forceinline__ void merge_shared_heads(const DecodeParams& P, Out* o
         int last = 0;
         if (n_ctas_s[e] > 1) {
             __threadfence();                                     // the CTA's states before its arrival (barrier above), the others' after it
-            last = atomicAdd(arrival_counters(P, shared_s[leader_s[e]].bh) + head, 1) == n_ctas_s[e] - 1;
+            last = atomicAdd(arrival_counters(P.qfrag, shared_s[leader_s[e]].bh) + head, 1) == n_ctas_s[e] - 1;
             __threadfence();
         }
         last_s[e][head] = last;
@@ -1286,7 +1225,7 @@ static bool make_plan(const CacheView& c, int batch, int max_seq_len, DecodePlan
 
 static cudaEvent_t g_prof_start = nullptr, g_prof_stop = nullptr;
 
-// selection: the kernel that fills P.selected goes between the preparation and the main kernel
+// selection: the kernel that fills P.selected prepares the queries too, in place of the preparation kernel
 template <int BITS, int MODE, bool SPARSE>
 static int launch_decode(const DecodeParams& P, int n_ctas, cudaStream_t st, const SelectParams* selection, int max_seq_len) {
     constexpr int MAIN_WARPS = main_warps(BITS, MODE);
@@ -1303,13 +1242,14 @@ static int launch_decode(const DecodeParams& P, int n_ctas, cudaStream_t st, con
     cfg.stream = st;
     cfg.attrs = pdl_attr;
     cfg.numAttrs = 1;
-    cfg.gridDim = dim3(P.c.n_kv, P.batch);
-    cfg.blockDim = dim3(PREP_THREADS);
-    cfg.dynamicSmemBytes = 0;
-    if (cudaLaunchKernelEx(&cfg, decode_prep_kernel<BITS, MODE>, P) != cudaSuccess) return WUSHKV_ECUDA;
     if (SPARSE && selection) {
         const int rc = launch_select(*selection, max_seq_len, st);
         if (rc != WUSHKV_OK) return rc;
+    } else {
+        cfg.gridDim = dim3(P.c.n_kv, P.batch);
+        cfg.blockDim = dim3(PREP_THREADS);
+        cfg.dynamicSmemBytes = 0;
+        if (cudaLaunchKernelEx(&cfg, decode_prep_kernel<BITS, MODE>, P) != cudaSuccess) return WUSHKV_ECUDA;
     }
     if (!opt_in_dynamic_smem(reinterpret_cast<const void*>(decode_main_kernel<BITS, MODE, STAGES, SPARSE>), static_cast<int>(SMEM))) return WUSHKV_ECUDA;
     if (g_prof_start) cudaEventRecord(g_prof_start, st);
@@ -1397,7 +1337,8 @@ static int decode_attn_impl(const wushkv_cache* cache, int32_t batch, const int3
             sel.bounds = reinterpret_cast<const signed char*>(sparse->bounds);
             sel.exponents = reinterpret_cast<const signed char*>(sparse->exponents);
             sel.n_select = sparse->n_select; sel.selected = sparse->selected;
-            sel.early = 1;       // every CTA of the preparation kernel has waited for all earlier work when this one may start
+            sel.qfrag = P.qfrag; sel.qwfrag = P.qwfrag; sel.qscal = P.qscal;
+            sel.plan = batch > MAX_LOCAL_PLAN ? P.plan : nullptr;
         }
         const SelectParams* selection = sparse->bounds ? &sel : nullptr;
         if (P.c.bits == 2) return mode0 ? launch_decode<2, 0, true>(P, pl.n_ctas, st, selection, max_seq_len) : launch_decode<2, 1, true>(P, pl.n_ctas, st, selection, max_seq_len);

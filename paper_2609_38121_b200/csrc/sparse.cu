@@ -23,6 +23,7 @@ namespace cg = cooperative_groups;
 constexpr unsigned FULL = 0xffffffffu;
 constexpr int MIN_EXPONENT = -31, MAX_EXPONENT = 14;      // of 2^e: fp16 steps and offsets reach from 2^-24 to 2^20
 constexpr double Q_MAX = 32512.0;                         // 127 * 256: both digits of the fixed-point query fit a signed byte
+constexpr float LOG2E = 1.4426950408889634f;
 
 // ------------------------------------------------------------------------------------------------
 // bounds
@@ -197,6 +198,7 @@ struct SelectShared {
     double q[8][D];                   // the queries, in 64 bits
     double qc[8][D];                  // q' of all CTAs' rows
     uint4 frag[2 * 4 * 32];           // B fragments: [digit set][64 bytes of bounds][lane]
+    uint4 attn[128 + 256];            // the attention's integer and bf16 fragments of the head
     uint4 bins[SELECT_THREADS];       // CTA 0: pages per bin of the range of keys
     float unit[8];                    // score of one unit of 2^e dot
     float warp_best[SELECT_WARPS][8];
@@ -290,7 +292,7 @@ __global__ void __launch_bounds__(SELECT_THREADS) select_pages_kernel(SelectPara
     const CacheView& c = P.c;
     const int rank = static_cast<int>(cluster.block_rank()), h = blockIdx.y, b = blockIdx.z;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3, G = c.G;
-    if (!P.early) pdl_wait();
+    pdl_wait();
     pdl_launch_dependents();
     // nobody writes into another CTA's shared memory before that CTA has come here and zeroed what the others add to
     if (tid == 0) { sh.most = 0u; sh.n_list = 0; }
@@ -316,12 +318,15 @@ __global__ void __launch_bounds__(SELECT_THREADS) select_pages_kernel(SelectPara
         }
     }
     const bool all = pages <= P.n_select;               // the same for the whole cluster
+    const bool prepare = P.qfrag != nullptr;
     if (all) {
         if (rank == 0)
             for (int i = tid; i < P.n_select; i += SELECT_THREADS) out[i] = i < pages ? first + i : -1;
-        if (CL > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-        if (P.early) pdl_wait();
-        return;
+        if (!prepare) {
+            if (CL > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+            return;
+        }
+        pages = 0;                                      // nothing to score
     }
     const int per_max = pages_per_cta(P.max_candidates, CL);
     float* scores = reinterpret_cast<float*>(select_smem + sizeof(SelectShared));            // [G][per_max]
@@ -337,7 +342,7 @@ __global__ void __launch_bounds__(SELECT_THREADS) select_pages_kernel(SelectPara
 #pragma unroll
     for (int k = 0; k < QUADS; ++k) { tr[0][k] = ld_early(T + seg + TPP * k); tr[1][k] = ld_early(T + PAIRS * (D / 4) + seg + TPP * k); }
     BoundsTile tile;
-    tile.load(P, table, h, p_lo + 16 * warp, p_hi, g, t);
+    if (!all) tile.load(P, table, h, p_lo + 16 * warp, p_hi, g, t);
     if (warp < GP) {
         float x[4] = {0.f, 0.f, 0.f, 0.f};              // slots without a head are zero
         if (warp < G) {
@@ -345,13 +350,15 @@ __global__ void __launch_bounds__(SELECT_THREADS) select_pages_kernel(SelectPara
             x[0] = bf16_bits_to_float(w.x & 0xffff); x[1] = bf16_bits_to_float(w.x >> 16);
             x[2] = bf16_bits_to_float(w.y & 0xffff); x[3] = bf16_bits_to_float(w.y >> 16);
             if (P.pro.rope)
-                norm_rope_warp(x, lane, P.pro, h * G + warp, prologue_position(P.pro, S - 1, c.dev_status, lane == 0 && rank == 0));
+                norm_rope_warp(x, lane, P.pro, h * G + warp, prologue_position(P.pro, max(S - 1, 0), c.dev_status, lane == 0 && rank == 0));
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) sh.q[warp][4 * lane + e] = static_cast<double>(x[e]);
     }
     sh.bins[tid] = make_uint4(0u, 0u, 0u, 0u);
     for (int i = tid; i < SETS * 4 * 32; i += SELECT_THREADS) sh.frag[i] = make_uint4(0u, 0u, 0u, 0u);      // columns without a head
+    if (prepare)
+        for (int i = tid; i < 128 + 256; i += SELECT_THREADS) sh.attn[i] = make_uint4(0u, 0u, 0u, 0u);
     __syncthreads();
     double acc[2 * GP];                                 // [row][head]
 #pragma unroll
@@ -398,10 +405,15 @@ __global__ void __launch_bounds__(SELECT_THREADS) select_pages_kernel(SelectPara
         const bool usable = most > 0.0 && most < 3e38;          // otherwise all scores are 0: the lowest pages
         const double per_unit = usable ? Q_MAX / most : 0.0;
         unsigned word[2][2] = {{0u, 0u}, {0u, 0u}};             // [lower, upper][high, low digit]
+        unsigned digits[2] = {0u, 0u};                          // the same of the attention: [high, low], a byte per channel
+        int sum = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int v = usable ? min(max(__double2int_rn(x[e] * per_unit), -32512), 32512) : 0;
             const int hi_digit = (v + 128) >> 8, lo_digit = v - 256 * hi_digit;
+            digits[0] |= static_cast<unsigned>(hi_digit & 255) << (8 * e);
+            digits[1] |= static_cast<unsigned>(lo_digit & 255) << (8 * e);
+            sum += v;
             const unsigned wh = static_cast<unsigned>(hi_digit & 255) << (8 * e), wl = static_cast<unsigned>(lo_digit & 255) << (8 * e);
             if (v > 0) { word[1][0] |= wh; word[1][1] |= wl; } else { word[0][0] |= wh; word[0][1] |= wl; }
         }
@@ -415,8 +427,51 @@ __global__ void __launch_bounds__(SELECT_THREADS) select_pages_kernel(SelectPara
                 frag[((set * 4 + group) * 32 + 4 * column + tl) * 4 + lane % 4] = word[side][digit];
             }
         if (lane == 0) sh.unit[warp] = usable ? static_cast<float>(__dmul_rn(most / Q_MAX, static_cast<double>(c.sm_scale))) : 0.f;
+        if (prepare && rank == CL - 1) {
+            // what decode_prep_kernel makes of q' (there from fp32 sums): digits in integer fragments, q' in the scale of the scores'
+            // base-2 exponent as bf16 value and remainder, two scalars per head
+            const float k2 = c.sm_scale * LOG2E, lam = usable ? static_cast<float>(most / Q_MAX) : 1.f;
+            unsigned short* ifrag = reinterpret_cast<unsigned short*>(sh.attn);
+            unsigned* wfrag = reinterpret_cast<unsigned*>(sh.attn + (MODE == 0 ? 64 : 128));
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {                       // channels ch, ch + 1
+                const int ch = 4 * lane + 2 * k, s = ch >> 5, hh = (ch >> 4) & 1, u = (ch >> 3) & 1, tq = (ch >> 1) & 3;
+#pragma unroll
+                for (int digit = 0; digit < 2; ++digit) {
+                    const int set = MODE == 0 ? 0 : digit, column = MODE == 0 ? 2 * warp + digit : warp;
+                    ifrag[set * 512 + (((s >> 1) * 32 + 4 * column + tq) * 16 + ((s & 1) * 2 + hh) * 4 + 2 * u) / 2] = static_cast<unsigned short>(digits[digit] >> (16 * k));
+                }
+                const int s16 = ch >> 4, r = (ch >> 3) & 1;
+                float y[2], rest[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    y[e] = static_cast<float>(x[2 * k + e]) * k2;
+                    rest[e] = y[e] - bf16_bits_to_float(float_to_bf16_bits(y[e]));
+                }
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    const int set = MODE == 0 ? 0 : part, column = MODE == 0 ? 2 * warp + part : warp;
+                    const float a = part == 0 ? y[0] : rest[0], d = part == 0 ? y[1] : rest[1];
+                    wfrag[set * 512 + ((s16 >> 1) * 32 + 4 * column + tq) * 4 + (s16 & 1) * 2 + r] = float_to_bf16_bits(a) | (static_cast<unsigned>(float_to_bf16_bits(d)) << 16);
+                }
+            }
+            sum = __reduce_add_sync(FULL, sum);
+            if (lane == 0) {
+                const float fs = c.bits != 4 ? 4.f : 16.f;      // the integer score of the main kernel carries this factor
+                reinterpret_cast<float2*>(P.qscal)[static_cast<long long>(b) * c.n_q + h * G + warp] = make_float2(k2 * lam / fs, fs * static_cast<float>(sum));
+            }
+        }
     }
     __syncthreads();
+    if (prepare && rank == CL - 1) {
+        constexpr int QF = MODE == 0 ? 64 : 128, QW = MODE == 0 ? 128 : 256;
+        const long long bh = static_cast<long long>(b) * c.n_kv + h;
+        if (tid < 8) arrival_counters(P.qfrag, bh)[tid] = 0;
+        if (tid < QF) P.qfrag[bh * 256 + tid] = sh.attn[tid];
+        if (tid < QW) P.qwfrag[bh * 256 + tid] = sh.attn[QF + tid];
+        if (P.plan && h == 0 && b == 0) write_plan(c, P.batch, P.seq_len, P.slot, P.n_select, P.plan);
+    }
+    if (all) return;
 
     // ---- scores of this CTA's pages
     uint4 bq[SETS][4];
@@ -579,14 +634,16 @@ __global__ void __launch_bounds__(SELECT_THREADS) select_pages_kernel(SelectPara
             else if (k == kth) { if (equal_before < room) out[below_before + equal_before] = first + p; ++equal_before; }
         }
     }
-    if (P.early) pdl_wait();
 }
+
+constexpr int SELECT_SMEM_MAX = 200 * 1024;
+static_assert(sizeof(SelectShared) + 4 * (8 * MAX_SELECT_PAGES / 8 + MAX_SELECT_PAGES) <= SELECT_SMEM_MAX, "clusters of 8 hold every allowed number of pages");
 
 template <int MODE, int CL>
 static int launch_select_cl(const SelectParams& P, cudaStream_t st) {
     const auto kernel = select_pages_kernel<MODE, CL>;
     const size_t smem = sizeof(SelectShared) + sizeof(float) * (static_cast<size_t>(P.c.G) * pages_per_cta(P.max_candidates, CL) + P.max_candidates);
-    if (!opt_in_dynamic_smem(reinterpret_cast<const void*>(kernel), 227 * 1024)) return WUSHKV_ECUDA;
+    if (!opt_in_dynamic_smem(reinterpret_cast<const void*>(kernel), SELECT_SMEM_MAX)) return WUSHKV_ECUDA;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -613,8 +670,7 @@ int launch_select(SelectParams P, int max_seq_len, cudaStream_t stream) {
     while (knobs().select_cluster == 0 && cl < 8 && clusters * cl < sm_count() && most > static_cast<long long>(cl) * 16 * SELECT_WARPS) cl *= 2;
     // the scores and the keys have to fit in shared memory
     const auto smem = [&](int k) { return sizeof(SelectShared) + sizeof(float) * (static_cast<size_t>(P.c.G) * pages_per_cta(P.max_candidates, k) + most); };
-    while (cl < 8 && smem(cl) > 227 * 1024) cl *= 2;
-    if (smem(cl) > 227 * 1024) return WUSHKV_ECAPACITY;
+    while (cl < 8 && smem(cl) > SELECT_SMEM_MAX) cl *= 2;
     const bool mode0 = P.c.G <= 4;
     switch (cl) {
         case 1: return mode0 ? launch_select_cl<0, 1>(P, stream) : launch_select_cl<1, 1>(P, stream);
@@ -657,6 +713,7 @@ extern "C" int wushkv_select_pages(const wushkv_cache* cache, int32_t batch, con
     if (prologue && !make_prologue(prologue, prologue->q_norm_weight, P.pro)) return WUSHKV_EINVAL;
     P.batch = batch; P.slot = slot; P.seq_len = seq_len; P.Q = Q;
     P.bounds = reinterpret_cast<const signed char*>(bounds); P.exponents = reinterpret_cast<const signed char*>(exponents);
-    P.n_select = n_select; P.selected = selected; P.early = 0;
+    P.n_select = n_select; P.selected = selected;
+    P.qfrag = P.qwfrag = nullptr; P.qscal = nullptr; P.plan = nullptr;
     return launch_select(P, max_seq_len, static_cast<cudaStream_t>(stream));
 }
