@@ -404,11 +404,11 @@ int wushkv_decode_step_host(const wushkv_cache* cache, int32_t batch, const int3
  *   be distinct; -1 is skipped, an index outside the sequence's packed pages is skipped and flagged with BAD_PAGE_ID.  Positions
  *   of a listed page that a window holds are read from the window, as always.  Lists need not come from wushkv_select_pages.
  *   O (device, out): bf16 [batch][n_q][d], 16-byte aligned (the rounding is smaller than what a selection leaves out).
- * wushkv_decode_attn_sparse is both in one call, the selection running beside the preparation of the queries.
+ * wushkv_decode_attn_sparse is both in one launch.  selected may be NULL there: the list is then kept in workspace (device,
+ * 256-byte aligned, >= wushkv_sparse_workspace_bytes() bytes, scratch), which is not used otherwise and may then be NULL.
  * prologue: NULL, or the Norm / RoPE of projected queries (as in wushkv_decode_attn_projected).
- * The other arguments are those of wushkv_decode_attn; workspace: >= wushkv_sparse_workspace_bytes() bytes, 256-byte aligned,
- * scratch.  A sequence may be named by several rows of a call with different lengths (tokens to verify), as long as the ring
- * still holds the recent window of the shortest.
+ * The other arguments are those of wushkv_decode_attn.  A sequence may be named by several rows of a call with different lengths
+ * (tokens to verify), as long as the ring still holds the recent window of the shortest.
  */
 int wushkv_update_page_bounds(const wushkv_cache* cache, int32_t batch, const int32_t* slot, const int32_t* seq_len,
                               const int32_t* cu_new, int32_t max_new, int8_t* bounds, int8_t* exponents, void* stream);
@@ -418,7 +418,7 @@ int wushkv_select_pages(const wushkv_cache* cache, int32_t batch, const int32_t*
 size_t wushkv_sparse_workspace_bytes(const wushkv_cache* cache, int32_t batch, int32_t max_seq_len, int32_t n_select);
 int wushkv_decode_attn_selected(const wushkv_cache* cache, int32_t batch, const int32_t* slot, const int32_t* seq_len, int32_t max_seq_len,
                                 const uint16_t* Q, const wushkv_prologue* prologue, const int32_t* selected, int32_t n_select,
-                                uint16_t* O, void* workspace, size_t workspace_bytes, void* stream);
+                                uint16_t* O, void* stream);
 int wushkv_decode_attn_sparse(const wushkv_cache* cache, int32_t batch, const int32_t* slot, const int32_t* seq_len, int32_t max_seq_len,
                               const uint16_t* Q, const wushkv_prologue* prologue, const int8_t* bounds, const int8_t* exponents,
                               int32_t n_select, int32_t* selected, uint16_t* O, void* workspace, size_t workspace_bytes, void* stream);

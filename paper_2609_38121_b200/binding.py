@@ -143,7 +143,7 @@ def _load():
             ("wushkv_update_page_bounds", C.c_int, [cache, i32, ptr, ptr, ptr, i32, ptr, ptr, ptr]),
             ("wushkv_select_pages", C.c_int, [cache, i32, ptr, ptr, i32, ptr, prologue, ptr, ptr, i32, ptr, ptr]),
             ("wushkv_sparse_workspace_bytes", size, [cache, i32, i32, i32]),
-            ("wushkv_decode_attn_selected", C.c_int, [cache, i32, ptr, ptr, i32, ptr, prologue, ptr, i32, ptr, ptr, size, ptr]),
+            ("wushkv_decode_attn_selected", C.c_int, [cache, i32, ptr, ptr, i32, ptr, prologue, ptr, i32, ptr, ptr]),
             ("wushkv_decode_attn_sparse", C.c_int, [cache, i32, ptr, ptr, i32, ptr, prologue, ptr, ptr, i32, ptr, ptr, ptr, size, ptr]),
             ("wushkv_pages_workspace_bytes", size, [pool, i32]),
             ("wushkv_pages_reserve", C.c_int, [pool, i32, ptr, ptr, ptr, ptr, ptr, ptr, ptr, size, ptr]),
@@ -398,17 +398,17 @@ def sparse_workspace_bytes(cache: wushkv_cache, batch: int, max_seq_len: int, n_
     return int(lib.wushkv_sparse_workspace_bytes(C.byref(cache), batch, max_seq_len, n_select))
 
 
-def decode_attn_selected(cache: wushkv_cache, batch, slot, seq_len, max_seq_len, Q, selected, n_select, O, workspace, workspace_bytes,
-                         prologue=None, stream=None):
+def decode_attn_selected(cache: wushkv_cache, batch, slot, seq_len, max_seq_len, Q, selected, n_select, O, prologue=None, stream=None):
     """wushkv_decode_attn_selected: attention over the windows and the listed pages; O bf16 [batch][n_q][d]."""
     _check(lib.wushkv_decode_attn_selected(C.byref(cache), batch, _ptr(slot), _ptr(seq_len), max_seq_len, _ptr(Q),
-                                           _prologue_ptr(prologue), _ptr(selected), n_select, _ptr(O), _ptr(workspace), workspace_bytes,
-                                           _stream_ptr(stream)), "wushkv_decode_attn_selected")
+                                           _prologue_ptr(prologue), _ptr(selected), n_select, _ptr(O), _stream_ptr(stream)),
+           "wushkv_decode_attn_selected")
 
 
-def decode_attn_sparse(cache: wushkv_cache, batch, slot, seq_len, max_seq_len, Q, bounds, exponents, n_select, selected, O, workspace,
-                       workspace_bytes, prologue=None, stream=None):
-    """wushkv_decode_attn_sparse: select_pages (into ``selected``) and decode_attn_selected in one call."""
+def decode_attn_sparse(cache: wushkv_cache, batch, slot, seq_len, max_seq_len, Q, bounds, exponents, n_select, selected, O, workspace=None,
+                       workspace_bytes=0, prologue=None, stream=None):
+    """wushkv_decode_attn_sparse: select_pages and decode_attn_selected in one launch.  ``selected`` None: the list is kept in
+    ``workspace``, which is not needed otherwise."""
     _check(lib.wushkv_decode_attn_sparse(C.byref(cache), batch, _ptr(slot), _ptr(seq_len), max_seq_len, _ptr(Q), _prologue_ptr(prologue),
                                          _ptr(bounds), _ptr(exponents), n_select, _ptr(selected), _ptr(O), _ptr(workspace),
                                          workspace_bytes, _stream_ptr(stream)), "wushkv_decode_attn_sparse")

@@ -117,9 +117,15 @@ class Sparse:
             alone = torch.full_like(sel, -9)
             B.select_pages(c, batch, slot, seq_len, longest, Q, self.bounds, self.exponents, n_select, alone, prologue=prologue)
             assert torch.equal(sel, alone)
+            again = torch.full_like(out, float("nan"))           # the list in the workspace
+            B.decode_attn_sparse(c, batch, slot, seq_len, longest, Q, self.bounds, self.exponents, n_select, None, again, ws, need, prologue=prologue)
+            assert torch.equal(out.view(torch.int16), again.view(torch.int16))
+            again.fill_(float("nan"))                            # the list handed over
+            B.decode_attn_selected(c, batch, slot, seq_len, longest, Q, sel, n_select, again, prologue=prologue)
+            self.by_list = again.float().cpu().numpy().astype(np.float64)
         else:
             sel = torch.as_tensor(np.ascontiguousarray(selected, dtype=np.int32)).cuda()
-            B.decode_attn_selected(c, batch, slot, seq_len, longest, Q, sel, n_select, out, ws, need, prologue=prologue)
+            B.decode_attn_selected(c, batch, slot, seq_len, longest, Q, sel, n_select, out, prologue=prologue)
         torch.cuda.synchronize()
         return sel.cpu().numpy(), out.float().cpu().numpy().astype(np.float64)
 
@@ -244,9 +250,9 @@ def test_lists_of_the_caller():
         _close(out[b], s.oracle_attention(b, q[b], lists[b]))
     assert s.L.cache.status() == 0
     # an index outside the packed pages is skipped and flagged; the others count
-    lists[0, 0, 1], lists[0, 1, 6] = 24, 1 << 30
+    lists[0, 0, 1], lists[0, 1, 6], lists[2, 0, 3] = 24, 1 << 30, -2
     _, out = s.sparse(Q, 7, selected=lists)
-    lists[0, 0, 1], lists[0, 1, 6] = -1, -1
+    lists[0, 0, 1], lists[0, 1, 6], lists[2, 0, 3] = -1, -1, -1
     for b in range(3):
         _close(out[b], s.oracle_attention(b, q[b], lists[b]))
     assert s.L.cache.status() == s.B.DEV_BAD_PAGE_ID
@@ -318,6 +324,25 @@ def test_bad_slots_tables_and_lengths_are_flagged():
     s.L.cache.dev_status.zero_()
     sel, _ = s.sparse(Q, 4, max_seq_len=700)
     assert s.L.cache.status() & s.B.DEV_BAD_COUNT and sel[1:].max() < 11
+
+
+@pytest.mark.parametrize("bits", [2, 3, 4])
+def test_a_copy_that_never_arrives_is_flagged_and_the_next_call_is_healthy(bits):
+    s = Sparse([2000, 1500], 8, 2, bits, seed=23)
+    q, Q = s.queries()
+    want = s.sparse(Q, 9)
+    try:
+        s.B.set_test_option("drop_copy_unit", 3)
+        s.B.set_test_option("wait_limit", 64)
+        _, out = s.sparse(Q, 9)
+    finally:
+        s.B.set_test_option("drop_copy_unit", -1)
+        s.B.set_test_option("wait_limit", 0)
+    assert s.L.cache.status() == s.B.DEV_COPY_TIMEOUT
+    assert np.array_equal(out[1], want[1][1]) and np.all(np.isfinite(out))
+    s.L.cache.dev_status.zero_()
+    sel, out = s.sparse(Q, 9)
+    assert s.L.cache.status() == 0 and np.array_equal(sel, want[0]) and np.array_equal(out, want[1])
 
 
 def test_nan_bounds_fields_and_damaged_tokens_stay_local():
