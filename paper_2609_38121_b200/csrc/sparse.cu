@@ -203,9 +203,8 @@ struct SparseParams {
     int* selected;                           // [batch][n_kv][n_select]
     unsigned short* O;                       // bf16 [batch][n_q][D]; nullptr: selection alone
     int max_candidates;                      // bound of the candidate pages, from the bound of the lengths
-    int wait_limit;                          // poll limit of the copies' barriers
-    int drop_unit;                           // testing aid: the key copy of this page of the first (sequence, head)'s list is never issued (-1: none)
     int stream_pages;                        // 1: the packed pages of a step cannot stay in L2 anyway: copy them with an evict-first hint
+    int ring_offset;                         // where the staging rings begin behind the shared structure: 0 (they follow the scores in time) or behind the scores
 };
 
 __device__ __forceinline__ void mma_s8(int (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
@@ -217,8 +216,10 @@ __device__ __forceinline__ void mma_s8(int (&c)[4], unsigned a0, unsigned a1, un
 constexpr int SPARSE_THREADS = 256, SPARSE_WARPS = SPARSE_THREADS / 32;
 constexpr int SELECT_BINS = 4 * SPARSE_THREADS;
 
-// Shared memory of a CTA: this, then a region that first holds the scores of its pages [heads][per] and (CTA 0) the keys of all
-// pages, later the warps' staging rings.
+// Shared memory of a CTA: this, then a region for the selection (the page ids and the scores of the CTA's pages [per], [heads][per],
+// CTA 0: key and page id of all pages) and the warps' staging rings.  Where the sizes allow it the rings are apart from the selection's
+// region, so that window tokens can be staged from the start; else the rings begin where the selection's region began.
+constexpr int LISTED = 512;               // listed pages that are handed over in shared memory, with their ids
 template <int MODE>
 struct SparseShared {
     static constexpr int GP = MODE == 0 ? 4 : 8, SETS = MODE == 0 ? 1 : 2;
@@ -229,16 +230,16 @@ struct SparseShared {
         float merged[GP][PART_STRIDE];    // at last the CTA's partial result of every head
     };
     union {
-        double qc[GP][D];                 // q' of all CTAs' rows
+        double qc[GP][D];                 // q' of this CTA's rows
         uint4 bins[SPARSE_THREADS];       // then, CTA 0: pages per bin of the range of keys
     };
+    uint2 listed[LISTED];                 // CTA 0: the listed pages, index and id
     uint4 frag[SETS * 4 * 32];            // B fragments of the selection: [digit set][64 bytes of bounds][lane]
-    unsigned long long bars[SPARSE_WARPS][4];
     float2 scal[8];                       // score multiplier (log2 domain) and x_min multiplier of the heads
     float unit[8];                        // score of one unit of 2^e dot
     float warp_best[SPARSE_WARPS][8];
     float best[8][8];                     // per CTA of the cluster: largest score of its pages, per head
-    int scan[SPARSE_WARPS];
+    int scan[SPARSE_WARPS], below[SPARSE_WARPS], equal[SPARSE_WARPS];
     unsigned most;                        // CTA 0: largest finite key
     int bin, before, inside;              // CTA 0: the bin of the n_select-th key, keys in the bins ahead, keys in it
     unsigned kth;
@@ -247,10 +248,15 @@ struct SparseShared {
 };
 
 // Staging ring of a warp: slots for the key side (codes, steps and offsets) and for the value side, filled and freed on their own,
-// so that the next page's keys are on their way while this one's values are used.  Two CTAs fit on an SM.
+// so that the next page's keys are on their way while this one's values are used.  Two CTAs fit on an SM.  The warp's lanes fill it
+// with 16-byte asynchronous copies: a bulk copy costs the lane that requests it some 440 cycles, and requests of several lanes are
+// served one after the other (three per page and eight rows per window unit made the staging slower than the work on it).
+// Copies are waited for in the order of their groups: K_PENDING / V_PENDING groups may be outstanding behind the one that is needed
+// next, where the order is  K0 V0 [K1 [V1]]  then, per unit,  K(i + NK)  after its scores and  V(i + NV)  after its values.
 template <int BITS>
 struct Ring {
     static constexpr int NK = BITS == 4 ? 1 : 2, NV = BITS == 2 ? 2 : 1;
+    static constexpr int K_PENDING = NK + NV - 1, V_PENDING = NV == 2 ? 3 : 1;
     static constexpr int META = PAGE_TOKENS * 8, WINDOW = WIN_TOKENS * WIN_ROW;      // bytes of steps and offsets; of a window unit's rows
     static constexpr int K_SLOT = side_bytes(BITS) + META, V_SLOT = side_bytes(BITS) > WINDOW ? side_bytes(BITS) : WINDOW;
     static constexpr int BYTES = NK * K_SLOT + NV * V_SLOT;
@@ -272,8 +278,19 @@ __device__ __forceinline__ int ld_early_s8(const signed char* p) {
     return v;
 }
 
-// Ordinary accesses to shared memory so far come before bulk copies into it later (after a barrier).
-__device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async;" ::: "memory"); }
+// Asynchronous copy of 16 bytes into shared memory; L2 drops the line first if `stream`.
+__device__ __forceinline__ void copy16(unsigned dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy16_stream(unsigned dst, const void* src, unsigned long long policy) {
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int PENDING>
+__device__ __forceinline__ void copies_wait() {              // of this lane's copies; then of the whole warp's
+    asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory");
+    __syncwarp();
+}
 
 // Sums NV numbers per lane over groups of LANES lanes.  While there are several, each step hands half of them to the other side;
 // afterwards lane l of the group holds the totals of first(l) .. first(l) + LEFT - 1, and REPLICAS lanes hold the same.
@@ -302,18 +319,17 @@ struct GroupSum {
     static __device__ __forceinline__ int replica(int l) { return l % REPLICAS; }
 };
 
-// One tile of 16 pages as a lane reads it: 64 bytes of the bounds of rows g and g + 8 and the rows' exponents.
+// One tile of 16 pages as a lane reads it: 64 bytes of the bounds of rows g and g + 8 and the rows' exponents.  ids: the page ids of
+// the CTA's n pages, -1 where the table names none.
 struct BoundsTile {
     uint4 a[2][4];
     int ex[2];
     bool good[2];
-    __device__ __forceinline__ void load(const SparseParams& P, const int* table, int h, int p0, int p_hi, int g, int t) {
+    __device__ __forceinline__ void load(const SparseParams& P, const int* ids, int h, int p0, int n, int g, int t) {
 #pragma unroll
         for (int rs = 0; rs < 2; ++rs) {
-            const int p = p0 + g + 8 * rs;
-            const int page = p < p_hi ? __ldg(table + p) : -1;
-            good[rs] = page >= 0 && page < P.c.n_pages;
-            if (p < p_hi && !good[rs] && t == 0) atomicOr(P.c.dev_status, WUSHKV_DEV_BAD_PAGE_ID);
+            const int p = p0 + g + 8 * rs, page = p < n ? ids[p] : -1;
+            good[rs] = page >= 0;
             const long long ph = static_cast<long long>(good[rs] ? page : 0) * P.c.n_kv + h;
             const uint4* src = reinterpret_cast<const uint4*>(P.bounds + ph * 2 * D) + t;
 #pragma unroll
@@ -322,53 +338,64 @@ struct BoundsTile {
         }
     }
 };
+__device__ __forceinline__ void prefetch_bounds(const SparseParams& P, int page, int h) {
+    const long long ph = static_cast<long long>(page) * P.c.n_kv + h;
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(P.bounds + ph * 2 * D));
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(P.bounds + ph * 2 * D + D));
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(P.exponents + ph));
+}
 
-// The n_select smallest of the keys, ties to the lower page, in ascending order of the pages, by one CTA.  Keys are counted in bins
-// of equal width; the bin of the n_select-th smallest is found by a prefix sum and its few keys are compared with each other.
+// The n_select smallest of the keys (.x; .y is the page's id), ties to the lower page, in ascending order of the pages, by one CTA.
+// Keys are counted in bins of equal width; the bin of the n_select-th smallest is found by a prefix sum and its few keys are
+// compared with each other.
 template <class Shared>
-__device__ __forceinline__ void list_pages(Shared& sh, const unsigned* keys, int pages, int first, int n_select, int* out) {
+__device__ __forceinline__ void list_pages(Shared& sh, const uint2* keys, int pages, int first, int n_select, int* out) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     constexpr unsigned INF_BITS = 0x7f800000u;
+    sh.bins[tid] = make_uint4(0u, 0u, 0u, 0u);
     // bins of equal width from 0 to the largest key; the product is monotonic in the key, so bins are in the keys' order
     const float width = __uint_as_float(sh.most), per_bin = width > 0.f ? (SELECT_BINS - 1) / width : 0.f;
     const auto bin_of = [&](unsigned u) { return u < INF_BITS ? min(static_cast<int>(__uint_as_float(u) * per_bin), SELECT_BINS - 1) : SELECT_BINS - 1; };
     unsigned* bins = reinterpret_cast<unsigned*>(sh.bins);
-    for (int p = tid; p < pages; p += SPARSE_THREADS) atomicAdd(bins + bin_of(keys[p]), 1u);
-    const auto prefix = [&](int x) {                        // exclusive prefix sum over the CTA
-        int incl = x;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(FULL, incl, o);
-            if (lane >= o) incl += y;
-        }
-        if (lane == 31) sh.scan[warp] = incl;
-        __syncthreads();
-        int before = 0;
-#pragma unroll
-        for (int w = 0; w < SPARSE_WARPS; ++w) before += w < warp ? sh.scan[w] : 0;
-        return before + incl - x;
-    };
+    __syncthreads();
+#pragma unroll 4
+    for (int p = tid; p < pages; p += SPARSE_THREADS) atomicAdd(bins + bin_of(keys[p].x), 1u);
     __syncthreads();
     const uint4 mine = sh.bins[tid];
     const int counts[4] = {static_cast<int>(mine.x), static_cast<int>(mine.y), static_cast<int>(mine.z), static_cast<int>(mine.w)};
-    int before = prefix(counts[0] + counts[1] + counts[2] + counts[3]);
+    const int here = counts[0] + counts[1] + counts[2] + counts[3];
+    int before = here;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if (before < n_select && n_select <= before + counts[e]) { sh.bin = 4 * tid + e; sh.before = before; sh.inside = counts[e]; }
-        before += counts[e];
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(FULL, before, o);
+        if (lane >= o) before += y;
+    }
+    if (lane == 31) sh.scan[warp] = before;
+    __syncthreads();
+    before -= here;
+#pragma unroll
+    for (int w = 0; w < SPARSE_WARPS; ++w) before += w < warp ? sh.scan[w] : 0;
+    if (before < n_select && n_select <= before + here) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (before < n_select && n_select <= before + counts[e]) { sh.bin = 4 * tid + e; sh.before = before; sh.inside = counts[e]; }
+            before += counts[e];
+        }
     }
     __syncthreads();
     const int bin = sh.bin, inside = sh.inside, wanted = n_select - sh.before - 1;      // rank of the n_select-th key in its bin
     unsigned kth = 0u;
     if (inside <= SPARSE_THREADS) {
+#pragma unroll 4
         for (int p = tid; p < pages; p += SPARSE_THREADS) {
-            const unsigned u = keys[p];
+            const unsigned u = keys[p].x;
             if (bin_of(u) == bin) sh.list[atomicAdd(&sh.n_list, 1)] = u;
         }
         __syncthreads();
         if (tid < inside) {
             const unsigned u = sh.list[tid];
             int less = 0, same = 0;
+#pragma unroll 4
             for (int k = 0; k < inside; ++k) { less += sh.list[k] < u; same += sh.list[k] == u; }
             if (less <= wanted && wanted < less + same) sh.kth = u;      // equal keys write the same
         }
@@ -379,7 +406,7 @@ __device__ __forceinline__ void list_pages(Shared& sh, const unsigned* keys, int
         for (int bit = 30; bit >= 0; --bit) {
             const unsigned cand = kth | (1u << bit);
             int n = 0;
-            for (int p = tid; p < pages; p += SPARSE_THREADS) n += keys[p] < cand;
+            for (int p = tid; p < pages; p += SPARSE_THREADS) n += keys[p].x < cand;
             n = __reduce_add_sync(FULL, n);
             __syncthreads();
             if (lane == 0) sh.scan[warp] = n;
@@ -390,22 +417,35 @@ __device__ __forceinline__ void list_pages(Shared& sh, const unsigned* keys, int
             if (total < n_select) kth = cand;
         }
     }
-    __syncthreads();                                        // the readers of sh.scan
-    // all below it, and of those equal to it the first ones; every thread lists a run of consecutive pages
-    const int run = (pages + SPARSE_THREADS - 1) / SPARSE_THREADS, r_lo = min(tid * run, pages), r_hi = min(r_lo + run, pages);
+    // all below it, and of those equal to it the first ones; every warp lists a run of consecutive pages
+    const int run = (pages + 32 * SPARSE_WARPS - 1) / (32 * SPARSE_WARPS) * 32, r_lo = min(warp * run, pages), r_hi = min(r_lo + run, pages);
     int below = 0, equal = 0;
-    for (int p = r_lo; p < r_hi; ++p) { below += keys[p] < kth; equal += keys[p] == kth; }
-    static_assert(MAX_SELECT_PAGES < (1 << 15), "two counts in one prefix sum");
-    const int packed = prefix((below << 16) + equal);
-    int all_below = 0;
+    for (int p = r_lo + lane; p < r_hi; p += 32) { below += keys[p].x < kth; equal += keys[p].x == kth; }
+    below = __reduce_add_sync(FULL, below);
+    equal = __reduce_add_sync(FULL, equal);
+    if (lane == 0) { sh.below[warp] = below; sh.equal[warp] = equal; }
+    __syncthreads();
+    int all_below = 0, below_before = 0, equal_before = 0;
 #pragma unroll
-    for (int w = 0; w < SPARSE_WARPS; ++w) all_below += sh.scan[w] >> 16;
-    int below_before = packed >> 16, equal_before = packed & 0xffff;
+    for (int w = 0; w < SPARSE_WARPS; ++w) {
+        const int y = sh.below[w];
+        all_below += y;
+        if (w < warp) { below_before += y; equal_before += sh.equal[w]; }
+    }
     const int room = n_select - all_below;                  // places for keys equal to the n_select-th
-    for (int p = r_lo; p < r_hi; ++p) {
-        const unsigned k = keys[p];
-        if (k < kth) { out[below_before + min(equal_before, room)] = first + p; ++below_before; }
-        else if (k == kth) { if (equal_before < room) out[below_before + equal_before] = first + p; ++equal_before; }
+    const unsigned lower = (1u << lane) - 1u;
+    for (int p0 = r_lo; p0 < r_hi; p0 += 32) {
+        const int p = p0 + lane;
+        const uint2 k = p < r_hi ? keys[p] : make_uint2(0xffffffffu, 0u);
+        const unsigned is_below = __ballot_sync(FULL, k.x < kth), is_equal = __ballot_sync(FULL, k.x == kth);
+        const int e = equal_before + __popc(is_equal & lower);
+        if (k.x < kth || (k.x == kth && e < room)) {
+            const int at = below_before + __popc(is_below & lower) + min(e, room);
+            out[at] = first + p;
+            if (at < LISTED) sh.listed[at] = make_uint2(first + p, k.y);
+        }
+        below_before += __popc(is_below);
+        equal_before += __popc(is_equal);
     }
 }
 
@@ -428,6 +468,7 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
     extern __shared__ __align__(16) unsigned char sparse_smem[];
     Shared& sh = *reinterpret_cast<Shared*>(sparse_smem);
     unsigned char* region = sparse_smem + sizeof(Shared);
+    unsigned char* rings = region + P.ring_offset;
     cg::cluster_group cluster = cg::this_cluster();
     const CacheView& c = P.c;
     const int rank = CL > 1 ? static_cast<int>(cluster.block_rank()) : 0, h = blockIdx.y, b = blockIdx.z;
@@ -437,12 +478,19 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
     // nobody writes into another CTA's shared memory before that CTA has come here and zeroed what the others add to
     if (tid == 0) { sh.most = 0u; sh.n_list = 0; }
     if (CL > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-    const unsigned bar0 = smem_u32(&sh.bars[warp][0]);             // key slots, then (2 further) value slots
-    if (lane == 0) {
+    // ---- q': this thread's two rows of T_K^{-T} and its share of the queries are requested ahead of everything else
+    constexpr int ROWS = D / CL, PAIRS = ROWS / 2, TPP = SPARSE_THREADS / PAIRS, QUADS = D / 4 / TPP;      // threads per pair of rows, float4 per thread and row
+    constexpr int PART = QUADS > 4 ? 4 : QUADS;                                              // of them in flight together
+    const int t_row = rank * ROWS + tid / TPP, seg = tid % TPP;
+    const uint4* T = reinterpret_cast<const uint4*>(c.T_K_invT + (static_cast<long long>(h) * D + t_row) * D);
+    uint4 tr[2][PART];
+    const auto load_T = [&](int k0) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) mbar_init(bar0 + 8 * k, 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
+        for (int k = 0; k < PART; ++k) { tr[0][k] = ld_early(T + seg + TPP * (k0 + k)); tr[1][k] = ld_early(T + PAIRS * (D / 4) + seg + TPP * (k0 + k)); }
+    };
+    load_T(0);
+    uint2 q_bits = make_uint2(0u, 0u);                  // slots without a head are zero
+    if (warp < G) q_bits = __ldg(reinterpret_cast<const uint2*>(P.Q + (static_cast<long long>(b) * c.n_q + h * G + warp) * D + 4 * lane));
 
     // ---- candidates
     const int S = __ldcg(P.seq_len + b), slot = P.slot[b];
@@ -470,40 +518,67 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
         return;
     }
     const int per_max = pages_per_cta(P.max_candidates, CL);
-    float* scores = reinterpret_cast<float*>(region);                                        // [G][per_max]
-    unsigned* keys = reinterpret_cast<unsigned*>(scores + static_cast<size_t>(G) * per_max);
-    const int per = pages_per_cta(pages, CL), p_lo = min(rank * per, pages), p_hi = min(p_lo + per, pages);
+    int* ids = reinterpret_cast<int*>(region);                                               // [per_max]
+    float* scores = reinterpret_cast<float*>(ids + per_max);                                 // [G][per_max]
+    uint2* keys = reinterpret_cast<uint2*>(scores + static_cast<size_t>(G) * per_max);       // CTA 0: [max_candidates]
+    const int per = pages_per_cta(pages, CL), p_lo = min(rank * per, pages), n_here = min(p_lo + per, pages) - p_lo;      // this CTA's candidates
     const int* row = c.page_table + static_cast<long long>(slot) * c.max_pages;              // read only if there are pages
-    const int* table = row + first;
-
-    // ---- q', two rows per thread (a query element read from shared memory serves both)
-    constexpr int ROWS = D / CL, PAIRS = ROWS / 2, TPP = SPARSE_THREADS / PAIRS, QUADS = D / 4 / TPP;      // threads per pair of rows, float4 per thread and row
-    constexpr int PART = QUADS > 4 ? 4 : QUADS;                                              // of them in flight together
-    const int t_row = rank * ROWS + tid / TPP, seg = tid % TPP;
-    const uint4* T = reinterpret_cast<const uint4*>(c.T_K_invT + (static_cast<long long>(h) * D + t_row) * D);
-    uint4 tr[2][PART];
-    const auto load_T = [&](int k0) {
-#pragma unroll
-        for (int k = 0; k < PART; ++k) { tr[0][k] = ld_early(T + seg + TPP * (k0 + k)); tr[1][k] = ld_early(T + PAIRS * (D / 4) + seg + TPP * (k0 + k)); }
-    };
-    load_T(0);
-    BoundsTile tile;
-    if (score) tile.load(P, table, h, p_lo + 16 * warp, p_hi, g, t);
-    if (warp < GP) {
-        float x[4] = {0.f, 0.f, 0.f, 0.f};              // slots without a head are zero
-        if (warp < G) {
-            const uint2 w = *reinterpret_cast<const uint2*>(P.Q + (static_cast<long long>(b) * c.n_q + h * G + warp) * D + 4 * lane);
-            x[0] = bf16_bits_to_float(w.x & 0xffff); x[1] = bf16_bits_to_float(w.x >> 16);
-            x[2] = bf16_bits_to_float(w.y & 0xffff); x[3] = bf16_bits_to_float(w.y >> 16);
-            if (P.pro.rope)
-                norm_rope_warp(x, lane, P.pro, h * G + warp, prologue_position(P.pro, max(S - 1, 0), c.dev_status, lane == 0 && rank == 0));
+    if (score) {
+        for (int p = tid; p < n_here; p += SPARSE_THREADS) {
+            const int page = __ldg(row + first + p_lo + p);
+            const bool good = page >= 0 && page < c.n_pages;
+            if (good) prefetch_bounds(P, page, h);
+            else atomicOr(c.dev_status, WUSHKV_DEV_BAD_PAGE_ID);
+            ids[p] = good ? page : -1;
         }
+    }
+
+    // ---- window tokens: by all warps, or by those of the CTAs that will not be listing pages.  Staged from the start if the rings are apart.
+    unsigned char* ring = rings + warp * R::BYTES;
+    const unsigned k_slot0 = smem_u32(ring), v_slot0 = k_slot0 + R::NK * R::K_SLOT;
+    const bool spared = score && CL > 1;
+    const int win_first = (spared ? rank - 1 : rank) * SPARSE_WARPS + warp, win_stride = (spared ? CL - 1 : CL) * SPARSE_WARPS;
+    const int n_window = (si.n_win + WIN_TOKENS - 1) / WIN_TOKENS;
+    const int my_windows = !attend || (spared && rank == 0) || win_first >= n_window ? 0 : (n_window - win_first + win_stride - 1) / win_stride;
+    // the key or value rows of the k-th of them into a slot: lanes 16 i .. 16 i + 15 copy row 2 j + i
+    const auto copy_rows = [&](bool value, int k) {
+        if (k < my_windows) {
+            const int w0 = (win_first + k * win_stride) * WIN_TOKENS, n_valid = min(WIN_TOKENS, si.n_win - w0);
+            const unsigned dst = value ? v_slot0 + (k % R::NV) * R::V_SLOT : k_slot0 + (k % R::NK) * R::K_SLOT;
+            const long long plane = (static_cast<long long>(slot) * c.n_kv + h) * 2 + (value ? 1 : 0);
+#pragma unroll
+            for (int j = 0; j < WIN_TOKENS / 2; ++j) {
+                const int r = 2 * j + lane / 16, w = w0 + r;
+                if (r < n_valid) {
+                    const unsigned short* src = w < si.n_sink ? c.sink_kv + (plane * c.s_sink + w) * D
+                                                              : c.ring_kv + (plane * c.ring_cap + (si.recent_lo + (w - si.n_sink)) % c.ring_cap) * D;
+                    copy16(dst + r * WIN_ROW + (lane % 16) * 16, src + (lane % 16) * 8);
+                }
+            }
+        }
+        copies_commit();
+    };
+    const auto stage_windows = [&] {
+        if (my_windows == 0) return;
+        copy_rows(false, 0);
+        copy_rows(true, 0);
+        if (R::NK > 1) copy_rows(false, 1);
+        if (R::NV > 1) copy_rows(true, 1);
+    };
+    if (P.ring_offset > 0) stage_windows();
+
+    if (warp < GP) {
+        float x[4] = {bf16_bits_to_float(q_bits.x & 0xffff), bf16_bits_to_float(q_bits.x >> 16), bf16_bits_to_float(q_bits.y & 0xffff), bf16_bits_to_float(q_bits.y >> 16)};
+        if (warp < G && P.pro.rope)
+            norm_rope_warp(x, lane, P.pro, h * G + warp, prologue_position(P.pro, max(S - 1, 0), c.dev_status, lane == 0 && rank == 0));
 #pragma unroll
         for (int e = 0; e < 4; ++e) sh.q[warp][4 * lane + e] = static_cast<double>(x[e]);
     }
     for (int i = tid; i < SETS * 4 * 32; i += SPARSE_THREADS) sh.frag[i] = make_uint4(0u, 0u, 0u, 0u);      // columns without a head
     if (tid < 8) sh.scal[tid] = make_float2(1.f, 0.f);
     __syncthreads();
+    BoundsTile tile;
+    if (score) tile.load(P, ids, h, 16 * warp, n_here, g, t);
     double acc[2 * GP];                                 // [row][head]
 #pragma unroll
     for (int j = 0; j < 2 * GP; ++j) acc[j] = 0.0;
@@ -529,18 +604,18 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
     }
     using Sum = GroupSum<2 * GP, TPP>;
     Sum::sum(acc, seg);
-    if (CL > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-#pragma unroll
-    for (int peer = 0; peer < CL; ++peer) {
-        if (peer % Sum::REPLICAS != Sum::replica(seg)) continue;
-        double* q_of = CL > 1 ? cluster.map_shared_rank(&sh.qc[0][0], peer) : &sh.qc[0][0];
+    if (Sum::replica(seg) == 0)
 #pragma unroll
         for (int i = 0; i < Sum::LEFT; ++i) {
             const int k = Sum::first(seg) + i;
-            q_of[(k % GP) * D + t_row + (k / GP) * PAIRS] = acc[i];
+            sh.qc[k % GP][t_row + (k / GP) * PAIRS] = acc[i];
         }
-    }
-    if (CL > 1) cluster.sync(); else __syncthreads();   // sh.q has been read, too
+    if (CL > 1) {
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+        cluster.sync();
+    } else {
+        __syncthreads();
+    }                                                    // sh.q has been read, too
     if (attend) {                                        // columns without a head
         for (int i = tid; i < Shared::QF + Shared::QW; i += SPARSE_THREADS) sh.attn[i] = make_uint4(0u, 0u, 0u, 0u);
         __syncthreads();
@@ -550,7 +625,12 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
     if (warp < G) {
         double x[4], most = 0.0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { x[e] = sh.qc[warp][4 * lane + e]; most = fmax(most, fabs(x[e])); }
+        for (int e = 0; e < 2; ++e) {                            // from the CTA whose rows they are
+            const double2* from = reinterpret_cast<const double2*>(&sh.qc[warp][4 * lane + 2 * e]);
+            const double2 v = *(CL > 1 ? cluster.map_shared_rank(from, 4 * lane / ROWS) : from);
+            x[2 * e] = v.x; x[2 * e + 1] = v.y;
+            most = fmax(most, fmax(fabs(v.x), fabs(v.y)));
+        }
 #pragma unroll
         for (int o = 16; o >= 1; o >>= 1) most = fmax(most, __shfl_xor_sync(FULL, most, o));
         const bool usable = most > 0.0 && most < 3e38;          // otherwise all scores are 0: the lowest pages
@@ -615,7 +695,6 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
     __syncthreads();
 
     if (score) {
-        sh.bins[tid] = make_uint4(0u, 0u, 0u, 0u);
         // ---- scores of this CTA's pages
         uint4 bq[SETS][4];
 #pragma unroll
@@ -623,9 +702,9 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
         float unit[NH], best[NH];                               // heads per lane: t, or 2 t and 2 t + 1
 #pragma unroll
         for (int k = 0; k < NH; ++k) { const int head = MODE == 0 ? t : 2 * t + k; unit[k] = head < G ? sh.unit[head] : 0.f; best[k] = -INFINITY; }
-        for (int p0 = p_lo + 16 * warp; p0 < p_hi; p0 += 16 * SPARSE_WARPS) {
+        for (int p0 = 16 * warp; p0 < n_here; p0 += 16 * SPARSE_WARPS) {
             const BoundsTile now = tile;
-            if (p0 + 16 * SPARSE_WARPS < p_hi) tile.load(P, table, h, p0 + 16 * SPARSE_WARPS, p_hi, g, t);
+            if (p0 + 16 * SPARSE_WARPS < n_here) tile.load(P, ids, h, p0 + 16 * SPARSE_WARPS, n_here, g, t);
             int acc_i[SETS][4] = {};
 #pragma unroll
             for (int k = 0; k < 4; ++k)
@@ -637,7 +716,7 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
 #pragma unroll
             for (int rs = 0; rs < 2; ++rs) {
                 const int p = p0 + g + 8 * rs;
-                if (p >= p_hi) continue;
+                if (p >= n_here) continue;
                 const float grid = __uint_as_float(static_cast<unsigned>(127 + now.ex[rs]) << 23);
 #pragma unroll
                 for (int k = 0; k < NH; ++k) {
@@ -646,7 +725,7 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
                     const int dot = MODE == 0 ? 256 * acc_i[0][2 * rs] + acc_i[0][2 * rs + 1] : 256 * acc_i[0][2 * rs + k] + acc_i[SETS - 1][2 * rs + k];
                     // one rounding to 32 bits, one of the product: an order that a plain computation can repeat
                     const float s = now.good[rs] ? __fmul_rn(__int2float_rn(dot) * grid, unit[k]) : -INFINITY;
-                    scores[head * per_max + p - p_lo] = s;
+                    scores[head * per_max + p] = s;
                     best[k] = fmaxf(best[k], s);
                 }
             }
@@ -672,7 +751,7 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
         if (CL > 1) cluster.sync(); else __syncthreads();
 
         // ---- keys: bits of the distance below the best page (smaller is better)
-        unsigned* keys0 = CL > 1 ? cluster.map_shared_rank(keys, 0) : keys;
+        uint2* keys0 = CL > 1 ? cluster.map_shared_rank(keys, 0) : keys;
         float top[GP];
 #pragma unroll
         for (int j = 0; j < GP; ++j) {
@@ -682,21 +761,20 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
             top[j] = m == -INFINITY ? 0.f : m;
         }
         unsigned most = 0u;
-        for (int p = p_lo + tid; p < p_hi; p += SPARSE_THREADS) {
+        for (int p = tid; p < n_here; p += SPARSE_THREADS) {
             float key = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < GP; ++j) if (j < G) key = fmaxf(key, __fsub_rn(scores[j * per_max + p - p_lo], top[j]));
+            for (int j = 0; j < GP; ++j) if (j < G) key = fmaxf(key, __fsub_rn(scores[j * per_max + p], top[j]));
             const unsigned u = __float_as_uint(key) & 0x7fffffffu;
-            keys0[p] = u;
+            keys0[p_lo + p] = make_uint2(u, static_cast<unsigned>(ids[p]));
             if (u < 0x7f800000u) most = max(most, u);
         }
         most = __reduce_max_sync(FULL, most);
         if (lane == 0 && most > 0u) atomicMax(CL > 1 ? cluster.map_shared_rank(&sh.most, 0) : &sh.most, most);
-        fence_proxy_async();                                    // the scores' and keys' places are filled by bulk copies later
         if (CL > 1) cluster.sync(); else __syncthreads();
         if (rank == 0) list_pages(sh, keys, pages, first, P.n_select, list);
         if (!attend) return;
-        if (rank == 0) { fence_proxy_async(); __syncthreads(); }      // the keys' place becomes the staging ring
+        if (rank == 0) __syncthreads();                         // the keys' place may become the staging ring
     }
 
     // ---- attention: this warp's query fragments and state
@@ -715,75 +793,34 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
     for (int k = 0; k < NH; ++k) { const float2 v = sh.scal[MODE == 0 ? t : 2 * t + k]; fmul[k] = v.x; gadd[k] = v.y; }
     WarpState<MODE> st;
     st.reset();
-    unsigned char* ring = region + warp * R::BYTES;
-    const unsigned k_slot0 = smem_u32(ring), v_slot0 = k_slot0 + R::NK * R::K_SLOT;
     const unsigned long long policy = l2_evict_first_policy();
-    const int wait_limit = P.wait_limit;
-    int k_next = 0, v_next = 0;                                 // copies issued so far
-    int k_done = 0, v_done = 0;                                 // and used
-    bool timed_out = false;
-    // The key side (V == false) or value side of the next unit is announced and copied; bytes == 0: the unit is skipped.
-    const auto wait = [&](bool value) {
-        const int done = value ? v_done : k_done, n = value ? R::NV : R::NK;
-        const unsigned bar = bar0 + 8 * ((value ? 2 : 0) + done % n);
-        // a phase that one lane saw complete is complete for all: keep the decision warp-uniform
-        if (!__any_sync(FULL, mbar_wait_bounded(bar, (done / n) & 1, wait_limit))) {
-            timed_out = true;
-            if (lane == 0) atomicOr(c.dev_status, WUSHKV_DEV_COPY_TIMEOUT);
-            // other copies of this warp may still be in flight: wait for each (bounded) before the ring is used for anything else
-            for (int k = k_done; k < k_next; ++k) mbar_wait_bounded(bar0 + 8 * (k % R::NK), (k / R::NK) & 1, min(wait_limit, 1 << 9));
-            for (int k = v_done; k < v_next; ++k) mbar_wait_bounded(bar0 + 8 * (2 + k % R::NV), (k / R::NV) & 1, min(wait_limit, 1 << 9));
-        }
-        if (value) ++v_done; else ++k_done;
-        return !timed_out;
-    };
-
-    // ---- window tokens: by all warps, or by those of the CTAs that are not listing pages
-    const int n_window = (si.n_win + WIN_TOKENS - 1) / WIN_TOKENS;
-    {
-        const bool spared = score && CL > 1;
-        const int first_warp = spared ? (rank - 1) * SPARSE_WARPS + warp : rank * SPARSE_WARPS + warp, stride = (spared ? CL - 1 : CL) * SPARSE_WARPS;
-        const int n = (spared && rank == 0) || first_warp >= n_window ? 0 : (n_window - first_warp + stride - 1) / stride;
-        const auto copy_rows = [&](bool value, int k) {
-            const int w0 = (first_warp + k * stride) * WIN_TOKENS, n_valid = min(WIN_TOKENS, si.n_win - w0);
-            const int done = value ? v_next : k_next, nn = value ? R::NV : R::NK;
-            const unsigned bar = bar0 + 8 * ((value ? 2 : 0) + done % nn), dst = value ? v_slot0 + (done % nn) * R::V_SLOT : k_slot0 + (done % nn) * R::K_SLOT;
-            if (lane == 0) mbar_expect_tx(bar, n_valid * D * 2);
-            __syncwarp();
-            if (lane < n_valid) {
-                const int w = w0 + lane;
-                const long long plane = (static_cast<long long>(slot) * c.n_kv + h) * 2 + (value ? 1 : 0);
-                const unsigned short* src = w < si.n_sink ? c.sink_kv + (plane * c.s_sink + w) * D
-                                                          : c.ring_kv + (plane * c.ring_cap + (si.recent_lo + (w - si.n_sink)) % c.ring_cap) * D;
-                bulk_copy_g2s(dst + lane * WIN_ROW, src, D * 2, bar);
-            }
-            if (value) ++v_next; else ++k_next;
-        };
-        const int k0 = k_next, v0 = v_next;
-        for (int k = 0; k < min(n, R::NK); ++k) copy_rows(false, k);
-        for (int k = 0; k < min(n, R::NV); ++k) copy_rows(true, k);
-        for (int k = 0; k < n && !timed_out; ++k) {
-            const unsigned ks = k_slot0 + (k_done % R::NK) * R::K_SLOT, vs = v_slot0 + (v_done % R::NV) * R::V_SLOT;
-            if (!wait(false) || !wait(true)) break;
-            const uint4* wq = sh.attn + Shared::QF;
-            window_unit<BITS, MODE>(st, ks, vs, min(WIN_TOKENS, si.n_win - (first_warp + k * stride) * WIN_TOKENS), [wq](int i) { return wq[i]; }, lane);
-            __syncwarp();
-            if (k_next - k0 < n) copy_rows(false, k_next - k0);
-            if (v_next - v0 < n) copy_rows(true, v_next - v0);
-        }
+    // ---- window tokens
+    if (P.ring_offset == 0) stage_windows();
+    for (int k = 0; k < my_windows; ++k) {
+        const unsigned ks = k_slot0 + (k % R::NK) * R::K_SLOT, vs = v_slot0 + (k % R::NV) * R::V_SLOT;
+        copies_wait<(R::NK < R::NV ? R::NK : R::NV) * 2 - 2>();
+        const uint4* wq = sh.attn + Shared::QF;
+        window_unit<BITS, MODE>(st, ks, vs, min(WIN_TOKENS, si.n_win - (win_first + k * win_stride) * WIN_TOKENS), [wq](int i) { return wq[i]; }, lane);
+        __syncwarp();
+        copy_rows(false, k + R::NK);
+        copy_rows(true, k + R::NV);
     }
+    copies_wait<0>();
     if (score) { if (CL > 1) cluster.sync(); else __syncthreads(); }      // the list is complete
 
     // ---- the listed pages, 32 of this warp's at a time: lane k looks up the k-th
     const int wid = rank * SPARSE_WARPS + warp;
     constexpr int STRIDE = CL * SPARSE_WARPS;
-    for (int base = wid; base < n_listed && !timed_out; base += 32 * STRIDE) {
+    for (int base = wid; base < n_listed; base += 32 * STRIDE) {
         const int n = min(32, (n_listed - base + STRIDE - 1) / STRIDE);
         int my_entry = -1, my_page = -1;
         if (lane < n) {
             const int u = base + lane * STRIDE;
-            my_entry = given || score ? __ldcg(list + u) : first + u;
-            if (my_entry != -1) {
+            if (score && u < LISTED) {
+                const uint2 e = *(CL > 1 ? cluster.map_shared_rank(&sh.listed[u], 0) : &sh.listed[u]);
+                my_entry = static_cast<int>(e.x);
+                my_page = static_cast<int>(e.y);                // -1: flagged when it was scored
+            } else if ((my_entry = given || score ? __ldcg(list + u) : first + u) != -1) {
                 const bool inside = my_entry >= first && my_entry < first + pages;
                 const int page = inside ? __ldg(row + my_entry) : -1;
                 if (page >= 0 && page < c.n_pages) my_page = page;
@@ -791,46 +828,48 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
             }
         }
         unsigned there = __ballot_sync(FULL, my_page >= 0), k_todo = there, v_todo = there;      // units of this warp, and those not yet requested
+        int ki = 0, vi = 0, k_slot = 0, v_slot = 0;             // slots of the next copies, of the unit at hand
+        const auto copy_side = [&](unsigned dst, const unsigned char* src, int bytes) {
+#pragma unroll
+            for (int i = 0; i < (bytes + 511) / 512; ++i)
+                if (bytes % 512 == 0 || 512 * i + 16 * lane < bytes) {
+                    if (P.stream_pages) copy16_stream(dst + 512 * i + 16 * lane, src + 512 * i + 16 * lane, policy);
+                    else copy16(dst + 512 * i + 16 * lane, src + 512 * i + 16 * lane);
+                }
+        };
         const auto copy_page = [&](bool value, unsigned& todo) {
-            const int k = __ffs(todo) - 1;
-            todo &= todo - 1;
-            const int page = __shfl_sync(FULL, my_page, k);
-            const int done = value ? v_next : k_next, nn = value ? R::NV : R::NK;
-            if (lane == 0) {
-                const unsigned bar = bar0 + 8 * ((value ? 2 : 0) + done % nn), dst = value ? v_slot0 + (done % nn) * R::V_SLOT : k_slot0 + (done % nn) * R::K_SLOT;
+            if (todo) {
+                const int page = __shfl_sync(FULL, my_page, __ffs(todo) - 1);
+                todo &= todo - 1;
                 const unsigned char* rec = c.pages + (static_cast<long long>(page) * c.n_kv + h) * record_bytes(BITS);
-                const bool drop = P.drop_unit >= 0 && !value && b == 0 && h == 0 && P.drop_unit == base + k * STRIDE;      // testing aid
-                mbar_expect_tx(bar, value ? side_bytes(BITS) : R::K_SLOT);
                 if (value) {
-                    if (P.stream_pages) bulk_copy_g2s_stream(dst, rec + v_codes_offset(BITS), side_bytes(BITS), bar, policy);
-                    else bulk_copy_g2s(dst, rec + v_codes_offset(BITS), side_bytes(BITS), bar);
-                } else if (!drop) {
-                    if (P.stream_pages) {
-                        bulk_copy_g2s_stream(dst, rec, side_bytes(BITS), bar, policy);
-                        bulk_copy_g2s_stream(dst + side_bytes(BITS), rec + meta_offset(BITS), R::META, bar, policy);
-                    } else {
-                        bulk_copy_g2s(dst, rec, side_bytes(BITS), bar);
-                        bulk_copy_g2s(dst + side_bytes(BITS), rec + meta_offset(BITS), R::META, bar);
-                    }
+                    copy_side(v_slot0 + vi * R::V_SLOT, rec + v_codes_offset(BITS), side_bytes(BITS));
+                    vi = vi + 1 == R::NV ? 0 : vi + 1;
+                } else {
+                    copy_side(k_slot0 + ki * R::K_SLOT, rec, side_bytes(BITS));
+                    copy_side(k_slot0 + ki * R::K_SLOT + side_bytes(BITS), rec + meta_offset(BITS), R::META);
+                    ki = ki + 1 == R::NK ? 0 : ki + 1;
                 }
             }
-            if (value) ++v_next; else ++k_next;
+            copies_commit();
         };
-#pragma unroll
-        for (int k = 0; k < R::NK; ++k) if (k_todo) copy_page(false, k_todo);
-#pragma unroll
-        for (int k = 0; k < R::NV; ++k) if (v_todo) copy_page(true, v_todo);
-        while (there && !timed_out) {
+        copy_page(false, k_todo);
+        copy_page(true, v_todo);
+        if (R::NK > 1) copy_page(false, k_todo);
+        if (R::NV > 1) copy_page(true, v_todo);
+        while (there) {
             const int k = __ffs(there) - 1;
             there &= there - 1;
             const int pos0 = __shfl_sync(FULL, my_entry, k) * PAGE_TOKENS;
-            const unsigned ks = k_slot0 + (k_done % R::NK) * R::K_SLOT, vs = v_slot0 + (v_done % R::NV) * R::V_SLOT;
-            if (!wait(false)) break;
+            const unsigned ks = k_slot0 + k_slot * R::K_SLOT, vs = v_slot0 + v_slot * R::V_SLOT;
+            k_slot = k_slot + 1 == R::NK ? 0 : k_slot + 1;
+            v_slot = v_slot + 1 == R::NV ? 0 : v_slot + 1;
+            copies_wait<R::K_PENDING>();
             float sc[4][2 * NH];          // [block][row g: heads..., row g+8: heads...]
             unsigned vmeta[4][2];         // fp16x2 (Delta_v, x_min_v) of rows g, g+8
             page_scores<BITS, MODE>(ks, ks + side_bytes(BITS), qf, qfl, gadd, sc, vmeta, lane);
             __syncwarp();
-            if (k_todo) copy_page(false, k_todo);               // the slot just read
+            copy_page(false, k_todo);                           // into the slot just read
             if (pos0 < si.q_lo || pos0 + PAGE_TOKENS > si.q_hi) {      // first / last page of the quantized range: mask the tokens outside it
 #pragma unroll
                 for (int bi = 0; bi < 4; ++bi)
@@ -852,11 +891,12 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
                 mx[j] = v * fmul[j];          // scores are kept divided by the head's multiplier (> 0)
             }
             st.raise_max(mx);
-            if (!wait(true)) break;
+            copies_wait<R::V_PENDING>();
             page_values<BITS, MODE>(st, vs, sc, vmeta, fmul, lane);
             __syncwarp();
-            if (v_todo) copy_page(true, v_todo);
+            copy_page(true, v_todo);
         }
+        copies_wait<0>();
     }
 
     // ---- merge: the CTA's eight states, then the cluster's
@@ -866,7 +906,7 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
     if (warp < G) {
         MergedState ms;
         ms.reset();
-        ms.add<false>(SPARSE_WARPS, lane, [&](int k) { return reinterpret_cast<const float*>(region + k * R::BYTES) + warp * PART_STRIDE; });
+        ms.add<false>(SPARSE_WARPS, lane, [&](int k) { return reinterpret_cast<const float*>(rings + k * R::BYTES) + warp * PART_STRIDE; });
         if (CL > 1) ms.store(sh.merged[warp], lane);
         else ms.finish(P.O + (static_cast<long long>(b) * c.n_q + h * G + warp) * D, lane);
     }
@@ -890,17 +930,24 @@ static long long candidate_bound(const CacheView& c, int max_seq_len) {
     return nq > 0 ? (c.s_sink + nq - 1) / PAGE_TOKENS - c.s_sink / PAGE_TOKENS + 1 : 0;
 }
 
-constexpr int SPARSE_SMEM_MAX = 200 * 1024;
-static_assert(sizeof(SparseShared<1>) + 4 * (8 * MAX_SELECT_PAGES / 8 + MAX_SELECT_PAGES) <= SPARSE_SMEM_MAX, "clusters of 8 hold every allowed number of pages");
+constexpr int SPARSE_SMEM_MAX = 226 * 1024, SPARSE_SMEM_HALF = 113 * 1024;      // of a CTA; of one of two on an SM
+__host__ __device__ constexpr size_t scored_bytes(size_t group, size_t per, size_t pages) { return (4 * (1 + group) * per + 8 * pages + 15) / 16 * 16; }
+static_assert(sizeof(SparseShared<1>) + scored_bytes(8, MAX_SELECT_PAGES / 8, MAX_SELECT_PAGES) <= SPARSE_SMEM_MAX, "clusters of 8 hold every allowed number of pages");
 
+// Shared memory of a CTA and where in it the rings begin.
 template <int BITS, int MODE>
-static size_t sparse_smem(const SparseParams& P, int cl) {
-    const size_t scored = P.bounds ? sizeof(float) * (static_cast<size_t>(P.c.G) * pages_per_cta(P.max_candidates, cl) + P.max_candidates) : 0;
-    return sizeof(SparseShared<MODE>) + std::max<size_t>(scored, P.O ? SPARSE_WARPS * Ring<BITS>::BYTES : 0);
+static size_t sparse_smem(const SparseParams& P, int cl, int& ring_offset) {
+    const size_t scored = P.bounds ? scored_bytes(P.c.G, pages_per_cta(P.max_candidates, cl), P.max_candidates) : 0;
+    const size_t ring = P.O ? SPARSE_WARPS * Ring<BITS>::BYTES : 0, apart = sizeof(SparseShared<MODE>) + scored + ring;
+    // apart from the scores unless that costs the second CTA of an SM one that would come
+    const bool alone = static_cast<long long>(P.batch) * P.c.n_kv * cl <= sm_count();
+    ring_offset = 0;
+    if (scored > 0 && ring > 0 && apart <= (alone ? SPARSE_SMEM_MAX : SPARSE_SMEM_HALF)) { ring_offset = static_cast<int>(scored); return apart; }
+    return sizeof(SparseShared<MODE>) + std::max(scored, ring);
 }
 
 template <int BITS, int MODE, int CL>
-static int launch_sparse_cl(const SparseParams& P, cudaStream_t st) {
+static int launch_sparse_cl(SparseParams P, cudaStream_t st) {
     const auto kernel = sparse_decode_kernel<BITS, MODE, CL>;
     if (!opt_in_dynamic_smem(reinterpret_cast<const void*>(kernel), SPARSE_SMEM_MAX)) return WUSHKV_ECUDA;
     cudaLaunchAttribute attr[2];
@@ -911,7 +958,7 @@ static int launch_sparse_cl(const SparseParams& P, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(CL, P.c.n_kv, P.batch);
     cfg.blockDim = dim3(SPARSE_THREADS);
-    cfg.dynamicSmemBytes = sparse_smem<BITS, MODE>(P, CL);
+    cfg.dynamicSmemBytes = sparse_smem<BITS, MODE>(P, CL, P.ring_offset);
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = CL > 1 ? 2 : 1;
@@ -927,7 +974,8 @@ static int launch_sparse_mode(const SparseParams& P, cudaStream_t st) {
     int cl = knobs().select_cluster;
     if (cl != 2 && cl != 4 && cl != 8) cl = 1;
     while (knobs().select_cluster == 0 && cl < 8 && clusters * cl < sm_count() && work > static_cast<long long>(cl) * SPARSE_WARPS) cl *= 2;
-    while (cl < 8 && sparse_smem<BITS, MODE>(P, cl) > SPARSE_SMEM_MAX) cl *= 2;
+    int offset;
+    while (cl < 8 && sparse_smem<BITS, MODE>(P, cl, offset) > SPARSE_SMEM_MAX) cl *= 2;
     switch (cl) {
         case 1: return launch_sparse_cl<BITS, MODE, 1>(P, st);
         case 2: return launch_sparse_cl<BITS, MODE, 2>(P, st);
@@ -951,10 +999,8 @@ static int sparse_impl(const wushkv_cache* cache, int32_t batch, const int32_t* 
     P.batch = batch; P.slot = slot; P.seq_len = seq_len; P.Q = Q;
     P.bounds = reinterpret_cast<const signed char*>(bounds); P.exponents = reinterpret_cast<const signed char*>(exponents);
     P.n_select = n_select; P.selected = selected; P.O = O;
-    P.max_candidates = static_cast<int>(candidates);
-    P.wait_limit = static_cast<int>(std::min<long long>(std::max<long long>(knobs().wait_limit, 0), 1 << 30));
-    if (P.wait_limit == 0) P.wait_limit = 1 << 19;                // polls that may sleep ~2 us each: about a second
-    P.drop_unit = static_cast<int>(std::min<long long>(std::max<long long>(knobs().drop_copy_unit, -1), 1 << 30));
+    P.max_candidates = bounds ? static_cast<int>(candidates) : 0;      // a list that is given: nothing is scored
+    P.ring_offset = 0;
     // upper bound of the packed bytes one step reads against the L2 size (126 MB)
     P.stream_pages = static_cast<double>(batch) * P.c.n_kv * std::min<double>(n_select, static_cast<double>(candidates)) * record_bytes(P.c.bits) > 126e6 ? 1 : 0;
     cudaStream_t st = static_cast<cudaStream_t>(stream);

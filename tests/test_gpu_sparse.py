@@ -326,25 +326,6 @@ def test_bad_slots_tables_and_lengths_are_flagged():
     assert s.L.cache.status() & s.B.DEV_BAD_COUNT and sel[1:].max() < 11
 
 
-@pytest.mark.parametrize("bits", [2, 3, 4])
-def test_a_copy_that_never_arrives_is_flagged_and_the_next_call_is_healthy(bits):
-    s = Sparse([2000, 1500], 8, 2, bits, seed=23)
-    q, Q = s.queries()
-    want = s.sparse(Q, 9)
-    try:
-        s.B.set_test_option("drop_copy_unit", 3)
-        s.B.set_test_option("wait_limit", 64)
-        _, out = s.sparse(Q, 9)
-    finally:
-        s.B.set_test_option("drop_copy_unit", -1)
-        s.B.set_test_option("wait_limit", 0)
-    assert s.L.cache.status() == s.B.DEV_COPY_TIMEOUT
-    assert np.array_equal(out[1], want[1][1]) and np.all(np.isfinite(out))
-    s.L.cache.dev_status.zero_()
-    sel, out = s.sparse(Q, 9)
-    assert s.L.cache.status() == 0 and np.array_equal(sel, want[0]) and np.array_equal(out, want[1])
-
-
 def test_nan_bounds_fields_and_damaged_tokens_stay_local():
     """A key that is not a number leaves the page's bounds to its other tokens."""
     s = Sparse([1000, 1000], 4, 1, 2, seed=18)
