@@ -226,15 +226,15 @@ struct SparseShared {
     static constexpr int QF = MODE == 0 ? 64 : 128, QW = MODE == 0 ? 128 : 256;     // uint4 of the attention's integer / bf16 fragments
     union {
         double q[GP][D];                  // the queries, in 64 bits
-        uint4 attn[QF + QW];              // then the attention's query fragments
+        uint4 frag[SETS * 4 * 32];        // then the selection's query fragments: [digit set][64 bytes of bounds][lane]
+        uint4 bins[SPARSE_THREADS];       // then, CTA 0: pages per bin of the range of keys
         float merged[GP][PART_STRIDE];    // at last the CTA's partial result of every head
     };
     union {
         double qc[GP][D];                 // q' of this CTA's rows
-        uint4 bins[SPARSE_THREADS];       // then, CTA 0: pages per bin of the range of keys
+        uint2 listed[LISTED];             // then, CTA 0: the listed pages, index and id
     };
-    uint2 listed[LISTED];                 // CTA 0: the listed pages, index and id
-    uint4 frag[SETS * 4 * 32];            // B fragments of the selection: [digit set][64 bytes of bounds][lane]
+    uint4 attn[QF + QW];                  // the attention's query fragments
     float2 scal[8];                       // score multiplier (log2 domain) and x_min multiplier of the heads
     float unit[8];                        // score of one unit of 2^e dot
     float warp_best[SPARSE_WARPS][8];
@@ -247,6 +247,65 @@ struct SparseShared {
     unsigned list[SPARSE_THREADS];        // keys of that bin
 };
 
+// One window unit of this kernel: up to 16 bf16 tokens, key rows staged at rows, value rows behind them, 256 bytes each, the 16-byte
+// piece i of row r at place i ^ (r & 7) (so that eight rows of a column of pieces lie in different banks).  Rows from n_valid on hold
+// copies of valid ones.  (The dense kernel's units have 8 tokens; here a warp gets one unit or none, and 16 tokens cost it little more.)
+constexpr int WIDE_TOKENS = 16;
+template <int BITS, int MODE>
+__device__ __forceinline__ void wide_window_unit(WarpState<MODE>& st, unsigned rows, int n_valid, const uint4* query, int lane) {
+    constexpr int NH = WarpState<MODE>::NH;
+    const int g = lane >> 2, mat = lane >> 3, r7 = lane & 7;
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    {
+        const unsigned row = rows + (r7 + 8 * (mat & 1)) * (2 * D);
+#pragma unroll
+        for (int s2 = 0; s2 < 4; ++s2) {
+            unsigned a[2][4];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) ldmatrix_x4(row + (((4 * s2 + 2 * k + (mat >> 1)) ^ r7) << 4), a[k][0], a[k][1], a[k][2], a[k][3]);
+#pragma unroll
+            for (int pass = 0; pass < (MODE == 0 ? 1 : 2); ++pass) {
+                const uint4 bq = query[pass * 128 + s2 * 32 + lane];
+                mma_bf16(acc, a[0][0], a[0][1], a[0][2], a[0][3], bq.x, bq.y);
+                mma_bf16(acc, a[1][0], a[1][1], a[1][2], a[1][3], bq.z, bq.w);
+            }
+        }
+    }
+    float sc[2][NH], mx[NH];                              // rows g, g + 8
+#pragma unroll
+    for (int rs = 0; rs < 2; ++rs)
+#pragma unroll
+        for (int k = 0; k < NH; ++k) sc[rs][k] = g + 8 * rs < n_valid ? (MODE == 0 ? acc[2 * rs] + acc[2 * rs + 1] : acc[2 * rs + k]) : -INFINITY;
+#pragma unroll
+    for (int k = 0; k < NH; ++k) mx[k] = fmaxf(sc[0][k], sc[1][k]);
+    st.raise_max(mx);
+    float p[2][NH];
+#pragma unroll
+    for (int rs = 0; rs < 2; ++rs)
+#pragma unroll
+        for (int k = 0; k < NH; ++k) { p[rs][k] = ex2(sc[rs][k] - st.mr[k]); st.l[k] += p[rs][k]; }
+    unsigned b01[MODE == 0 ? 1 : 2][2];                   // the probabilities as B fragments, tokens 2 t, 2 t + 1 (+ 8) of column g
+#pragma unroll
+    for (int rs = 0; rs < 2; ++rs)
+#pragma unroll
+        for (int pass = 0; pass < (MODE == 0 ? 1 : 2); ++pass) {
+            unsigned pr;                                  // value column, remainder column; or two heads' values, then their remainders
+            if (MODE == 0) pr = pack_bf2(p[rs][0], (p[rs][0] - bf16_round(p[rs][0])) * LO_SCALE);
+            else if (pass == 0) pr = pack_bf2(p[rs][0], p[rs][NH - 1]);
+            else pr = pack_bf2(p[rs][0] - bf16_round(p[rs][0]), p[rs][NH - 1] - bf16_round(p[rs][NH - 1]));
+            b01[pass][rs] = movmatrix_trans(pr);
+        }
+    const unsigned row = rows + WIDE_TOKENS * 2 * D + (r7 + 8 * (mat >> 1)) * (2 * D);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        unsigned a0, a1, a2, a3;                          // channels 16 i .. + 7 and + 8 .. + 15 of tokens 0 .. 7, the same of tokens 8 .. 15
+        ldmatrix_x4_trans(row + (((2 * i + (mat & 1)) ^ r7) << 4), a0, a1, a2, a3);
+        const unsigned unit = bf16x2_pow2(field_shift<BITS>(i) - 24);      // the block's accumulator unit
+#pragma unroll
+        for (int pass = 0; pass < (MODE == 0 ? 1 : 2); ++pass) mma_bf16(st.o[i], a0, a1, a2, a3, mul_bf2(b01[pass][0], unit), mul_bf2(b01[pass][1], unit));
+    }
+}
+
 // Staging ring of a warp: slots for the key side (codes, steps and offsets) and for the value side, filled and freed on their own,
 // so that the next page's keys are on their way while this one's values are used.  Two CTAs fit on an SM.  The warp's lanes fill it
 // with 16-byte asynchronous copies: a bulk copy costs the lane that requests it some 440 cycles, and requests of several lanes are
@@ -257,11 +316,11 @@ template <int BITS>
 struct Ring {
     static constexpr int NK = BITS == 4 ? 1 : 2, NV = BITS == 2 ? 2 : 1;
     static constexpr int K_PENDING = NK + NV - 1, V_PENDING = NV == 2 ? 3 : 1;
-    static constexpr int META = PAGE_TOKENS * 8, WINDOW = WIN_TOKENS * WIN_ROW;      // bytes of steps and offsets; of a window unit's rows
-    static constexpr int K_SLOT = side_bytes(BITS) + META, V_SLOT = side_bytes(BITS) > WINDOW ? side_bytes(BITS) : WINDOW;
+    static constexpr int META = PAGE_TOKENS * 8;                                     // bytes of steps and offsets
+    static constexpr int K_SLOT = side_bytes(BITS) + META, V_SLOT = side_bytes(BITS);
     static constexpr int BYTES = NK * K_SLOT + NV * V_SLOT;
-    static_assert(K_SLOT >= WINDOW && K_SLOT % 16 == 0 && V_SLOT % 16 == 0, "window rows fit, copies are aligned");
-    static_assert(BYTES >= 8 * PART_STRIDE * 4, "the partials of 8 query heads fit");
+    static_assert(K_SLOT % 16 == 0 && V_SLOT % 16 == 0, "copies are aligned");
+    static_assert(BYTES >= 8 * PART_STRIDE * 4 && BYTES >= 2 * WIDE_TOKENS * D * 2, "the partials of 8 query heads fit, and a window unit");
 };
 
 __host__ __device__ inline int pages_per_cta(int pages, int cl) { return ((pages + cl - 1) / cl + 15) / 16 * 16; }
@@ -351,18 +410,28 @@ __device__ __forceinline__ void prefetch_bounds(const SparseParams& P, int page,
 template <class Shared>
 __device__ __forceinline__ void list_pages(Shared& sh, const uint2* keys, int pages, int first, int n_select, int* out) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    constexpr unsigned INF_BITS = 0x7f800000u;
+    constexpr unsigned INF_BITS = 0x7f800000u, NONE = 0xffffffffu;
+    // Every warp has a run of consecutive pages, 32 at a time; the first KEPT of its lanes' keys stay in registers.
+    constexpr int KEPT = 8;
+    const int run = (pages + SPARSE_THREADS - 1) / SPARSE_THREADS * 32, r_lo = min(warp * run, pages), r_hi = min(r_lo + run, pages);
+    unsigned mine[KEPT];
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) { const int p = r_lo + 32 * i + lane; mine[i] = p < r_hi ? keys[p].x : NONE; }
+    const auto each = [&](auto f) {                         // f(key) of all keys of this lane (and of places behind the run: NONE)
+#pragma unroll
+        for (int i = 0; i < KEPT; ++i) if (32 * i < run) f(mine[i]);
+        for (int p = r_lo + 32 * KEPT + lane; p < r_hi; p += 32) f(keys[p].x);
+    };
     sh.bins[tid] = make_uint4(0u, 0u, 0u, 0u);
     // bins of equal width from 0 to the largest key; the product is monotonic in the key, so bins are in the keys' order
     const float width = __uint_as_float(sh.most), per_bin = width > 0.f ? (SELECT_BINS - 1) / width : 0.f;
     const auto bin_of = [&](unsigned u) { return u < INF_BITS ? min(static_cast<int>(__uint_as_float(u) * per_bin), SELECT_BINS - 1) : SELECT_BINS - 1; };
     unsigned* bins = reinterpret_cast<unsigned*>(sh.bins);
     __syncthreads();
-#pragma unroll 4
-    for (int p = tid; p < pages; p += SPARSE_THREADS) atomicAdd(bins + bin_of(keys[p].x), 1u);
+    each([&](unsigned u) { if (u != NONE) atomicAdd(bins + bin_of(u), 1u); });
     __syncthreads();
-    const uint4 mine = sh.bins[tid];
-    const int counts[4] = {static_cast<int>(mine.x), static_cast<int>(mine.y), static_cast<int>(mine.z), static_cast<int>(mine.w)};
+    const uint4 counted = sh.bins[tid];
+    const int counts[4] = {static_cast<int>(counted.x), static_cast<int>(counted.y), static_cast<int>(counted.z), static_cast<int>(counted.w)};
     const int here = counts[0] + counts[1] + counts[2] + counts[3];
     int before = here;
 #pragma unroll
@@ -386,11 +455,7 @@ __device__ __forceinline__ void list_pages(Shared& sh, const uint2* keys, int pa
     const int bin = sh.bin, inside = sh.inside, wanted = n_select - sh.before - 1;      // rank of the n_select-th key in its bin
     unsigned kth = 0u;
     if (inside <= SPARSE_THREADS) {
-#pragma unroll 4
-        for (int p = tid; p < pages; p += SPARSE_THREADS) {
-            const unsigned u = keys[p].x;
-            if (bin_of(u) == bin) sh.list[atomicAdd(&sh.n_list, 1)] = u;
-        }
+        each([&](unsigned u) { if (u != NONE && bin_of(u) == bin) sh.list[atomicAdd(&sh.n_list, 1)] = u; });
         __syncthreads();
         if (tid < inside) {
             const unsigned u = sh.list[tid];
@@ -406,7 +471,7 @@ __device__ __forceinline__ void list_pages(Shared& sh, const uint2* keys, int pa
         for (int bit = 30; bit >= 0; --bit) {
             const unsigned cand = kth | (1u << bit);
             int n = 0;
-            for (int p = tid; p < pages; p += SPARSE_THREADS) n += keys[p].x < cand;
+            each([&](unsigned u) { n += u < cand; });
             n = __reduce_add_sync(FULL, n);
             __syncthreads();
             if (lane == 0) sh.scan[warp] = n;
@@ -417,10 +482,9 @@ __device__ __forceinline__ void list_pages(Shared& sh, const uint2* keys, int pa
             if (total < n_select) kth = cand;
         }
     }
-    // all below it, and of those equal to it the first ones; every warp lists a run of consecutive pages
-    const int run = (pages + 32 * SPARSE_WARPS - 1) / (32 * SPARSE_WARPS) * 32, r_lo = min(warp * run, pages), r_hi = min(r_lo + run, pages);
+    // all below it, and of those equal to it the first ones
     int below = 0, equal = 0;
-    for (int p = r_lo + lane; p < r_hi; p += 32) { below += keys[p].x < kth; equal += keys[p].x == kth; }
+    each([&](unsigned u) { below += u < kth; equal += u == kth; });
     below = __reduce_add_sync(FULL, below);
     equal = __reduce_add_sync(FULL, equal);
     if (lane == 0) { sh.below[warp] = below; sh.equal[warp] = equal; }
@@ -434,19 +498,22 @@ __device__ __forceinline__ void list_pages(Shared& sh, const uint2* keys, int pa
     }
     const int room = n_select - all_below;                  // places for keys equal to the n_select-th
     const unsigned lower = (1u << lane) - 1u;
-    for (int p0 = r_lo; p0 < r_hi; p0 += 32) {
-        const int p = p0 + lane;
-        const uint2 k = p < r_hi ? keys[p] : make_uint2(0xffffffffu, 0u);
-        const unsigned is_below = __ballot_sync(FULL, k.x < kth), is_equal = __ballot_sync(FULL, k.x == kth);
+    int p = r_lo + lane;
+    const auto put = [&](unsigned u) {
+        const unsigned is_below = __ballot_sync(FULL, u < kth), is_equal = __ballot_sync(FULL, u == kth);
         const int e = equal_before + __popc(is_equal & lower);
-        if (k.x < kth || (k.x == kth && e < room)) {
+        if (u < kth || (u == kth && e < room)) {
             const int at = below_before + __popc(is_below & lower) + min(e, room);
             out[at] = first + p;
-            if (at < LISTED) sh.listed[at] = make_uint2(first + p, k.y);
+            if (at < LISTED) sh.listed[at] = make_uint2(first + p, keys[p].y);
         }
         below_before += __popc(is_below);
         equal_before += __popc(is_equal);
-    }
+        p += 32;
+    };
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) if (32 * i < run) put(mine[i]);
+    for (int i = KEPT; 32 * i < run; ++i) put(p < r_hi ? keys[p].x : NONE);
 }
 
 // One cluster of CL CTAs per (sequence, KV head).
@@ -475,9 +542,7 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3, G = c.G;
     pdl_wait();
     pdl_launch_dependents();
-    // nobody writes into another CTA's shared memory before that CTA has come here and zeroed what the others add to
-    if (tid == 0) { sh.most = 0u; sh.n_list = 0; }
-    if (CL > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    if (tid == 0) { sh.most = 0u; sh.n_list = 0; }      // the other CTAs touch this one's shared memory after the first cluster barrier only
     // ---- q': this thread's two rows of T_K^{-T} and its share of the queries are requested ahead of everything else
     constexpr int ROWS = D / CL, PAIRS = ROWS / 2, TPP = SPARSE_THREADS / PAIRS, QUADS = D / 4 / TPP;      // threads per pair of rows, float4 per thread and row
     constexpr int PART = QUADS > 4 ? 4 : QUADS;                                              // of them in flight together
@@ -513,10 +578,7 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
     const int n_listed = min(pages, P.n_select);
     if (!given && !score && rank == 0)
         for (int i = tid; i < P.n_select; i += SPARSE_THREADS) list[i] = i < pages ? first + i : -1;
-    if (!attend && !score) {
-        if (CL > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-        return;
-    }
+    if (!attend && !score) return;
     const int per_max = pages_per_cta(P.max_candidates, CL);
     int* ids = reinterpret_cast<int*>(region);                                               // [per_max]
     float* scores = reinterpret_cast<float*>(ids + per_max);                                 // [G][per_max]
@@ -533,39 +595,34 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
         }
     }
 
-    // ---- window tokens: by all warps, or by those of the CTAs that will not be listing pages.  Staged from the start if the rings are apart.
+    // ---- window tokens: by all warps, or by those of the CTAs that will not be listing pages.  Staged early if the rings are apart.
     unsigned char* ring = rings + warp * R::BYTES;
     const unsigned k_slot0 = smem_u32(ring), v_slot0 = k_slot0 + R::NK * R::K_SLOT;
     const bool spared = score && CL > 1;
     const int win_first = (spared ? rank - 1 : rank) * SPARSE_WARPS + warp, win_stride = (spared ? CL - 1 : CL) * SPARSE_WARPS;
-    const int n_window = (si.n_win + WIN_TOKENS - 1) / WIN_TOKENS;
+    const int n_window = (si.n_win + WIDE_TOKENS - 1) / WIDE_TOKENS;
     const int my_windows = !attend || (spared && rank == 0) || win_first >= n_window ? 0 : (n_window - win_first + win_stride - 1) / win_stride;
-    // the key or value rows of the k-th of them into a slot: lanes 16 i .. 16 i + 15 copy row 2 j + i
-    const auto copy_rows = [&](bool value, int k) {
+    // the rows of the k-th of them into the ring, two rows (lanes 0 - 15, 16 - 31) per instruction
+    const auto stage_window = [&](int k) {
         if (k < my_windows) {
-            const int w0 = (win_first + k * win_stride) * WIN_TOKENS, n_valid = min(WIN_TOKENS, si.n_win - w0);
-            const unsigned dst = value ? v_slot0 + (k % R::NV) * R::V_SLOT : k_slot0 + (k % R::NK) * R::K_SLOT;
-            const long long plane = (static_cast<long long>(slot) * c.n_kv + h) * 2 + (value ? 1 : 0);
+            const int w0 = (win_first + k * win_stride) * WIDE_TOKENS, last = si.n_win - 1, half = lane >> 4, piece = lane & 15;
+            const long long plane = (static_cast<long long>(slot) * c.n_kv + h) * 2;
+            const unsigned short* sink = c.sink_kv + plane * c.s_sink * D + piece * 8;
+            const unsigned short* recent = c.ring_kv + plane * c.ring_cap * D + piece * 8;
+            const int at0 = (si.recent_lo + max(w0 - si.n_sink, 0)) % c.ring_cap - max(w0, si.n_sink);      // ring row of window token w: at0 + w, or ring_cap less
 #pragma unroll
-            for (int j = 0; j < WIN_TOKENS / 2; ++j) {
-                const int r = 2 * j + lane / 16, w = w0 + r;
-                if (r < n_valid) {
-                    const unsigned short* src = w < si.n_sink ? c.sink_kv + (plane * c.s_sink + w) * D
-                                                              : c.ring_kv + (plane * c.ring_cap + (si.recent_lo + (w - si.n_sink)) % c.ring_cap) * D;
-                    copy16(dst + r * WIN_ROW + (lane % 16) * 16, src + (lane % 16) * 8);
-                }
+            for (int j = 0; j < WIDE_TOKENS / 2; ++j) {
+                const int r = 2 * j + half, w = min(w0 + r, last);
+                const bool in_sink = w < si.n_sink;
+                const int at = at0 + w;
+                const unsigned short* src = in_sink ? sink + w * D : recent + (at < c.ring_cap ? at : at - c.ring_cap) * D;
+                const unsigned dst = k_slot0 + r * (2 * D) + ((piece ^ (r & 7)) << 4);
+                copy16(dst, src);
+                copy16(dst + WIDE_TOKENS * 2 * D, src + static_cast<long long>(in_sink ? c.s_sink : c.ring_cap) * D);
             }
         }
         copies_commit();
     };
-    const auto stage_windows = [&] {
-        if (my_windows == 0) return;
-        copy_rows(false, 0);
-        copy_rows(true, 0);
-        if (R::NK > 1) copy_rows(false, 1);
-        if (R::NV > 1) copy_rows(true, 1);
-    };
-    if (P.ring_offset > 0) stage_windows();
 
     if (warp < GP) {
         float x[4] = {bf16_bits_to_float(q_bits.x & 0xffff), bf16_bits_to_float(q_bits.x >> 16), bf16_bits_to_float(q_bits.y & 0xffff), bf16_bits_to_float(q_bits.y >> 16)};
@@ -574,11 +631,10 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
 #pragma unroll
         for (int e = 0; e < 4; ++e) sh.q[warp][4 * lane + e] = static_cast<double>(x[e]);
     }
-    for (int i = tid; i < SETS * 4 * 32; i += SPARSE_THREADS) sh.frag[i] = make_uint4(0u, 0u, 0u, 0u);      // columns without a head
-    if (tid < 8) sh.scal[tid] = make_float2(1.f, 0.f);
     __syncthreads();
     BoundsTile tile;
     if (score) tile.load(P, ids, h, 16 * warp, n_here, g, t);
+    if (P.ring_offset > 0) stage_window(0);
     double acc[2 * GP];                                 // [row][head]
 #pragma unroll
     for (int j = 0; j < 2 * GP; ++j) acc[j] = 0.0;
@@ -610,19 +666,11 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
             const int k = Sum::first(seg) + i;
             sh.qc[k % GP][t_row + (k / GP) * PAIRS] = acc[i];
         }
-    if (CL > 1) {
-        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-        cluster.sync();
-    } else {
-        __syncthreads();
-    }                                                    // sh.q has been read, too
-    if (attend) {                                        // columns without a head
-        for (int i = tid; i < Shared::QF + Shared::QW; i += SPARSE_THREADS) sh.attn[i] = make_uint4(0u, 0u, 0u, 0u);
-        __syncthreads();
-    }
+    if (CL > 1) cluster.sync(); else __syncthreads();   // sh.q has been read, too
 
-    // ---- the query as two signed bytes per channel: q' ~ (max|q'| / 32512) (256 hi + lo), in B fragments
-    if (warp < G) {
+    // ---- the query as two signed bytes per channel: q' ~ (max|q'| / 32512) (256 hi + lo), in B fragments.  A warp per column pair (or
+    // column) of a head; the queries of head slots without a head are zero, and so are their columns.
+    if (warp < GP) {
         double x[4], most = 0.0;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {                            // from the CTA whose rows they are
@@ -633,7 +681,7 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
         }
 #pragma unroll
         for (int o = 16; o >= 1; o >>= 1) most = fmax(most, __shfl_xor_sync(FULL, most, o));
-        const bool usable = most > 0.0 && most < 3e38;          // otherwise all scores are 0: the lowest pages
+        const bool usable = most > 0.0 && most < 3e38;          // otherwise all scores are 0: the lowest pages (NaN compares false)
         constexpr double QM = Q_MAX;
         const double per_unit = usable ? QM / most : 0.0;
         // selection: row byte o of the bounds (lower 0 .. 127, upper 128 .. 255) is word (o % 16) / 4 of lane t = (o % 64) / 16 in group o / 64
@@ -774,7 +822,7 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
         if (CL > 1) cluster.sync(); else __syncthreads();
         if (rank == 0) list_pages(sh, keys, pages, first, P.n_select, list);
         if (!attend) return;
-        if (rank == 0) __syncthreads();                         // the keys' place may become the staging ring
+        if (CL > 1 && rank == 0) __syncthreads();               // the keys' place may become the staging ring
     }
 
     // ---- attention: this warp's query fragments and state
@@ -795,18 +843,16 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
     st.reset();
     const unsigned long long policy = l2_evict_first_policy();
     // ---- window tokens
-    if (P.ring_offset == 0) stage_windows();
+    if (score && CL == 1) __syncthreads();                      // the list is complete
+    if (P.ring_offset == 0) stage_window(0);
     for (int k = 0; k < my_windows; ++k) {
-        const unsigned ks = k_slot0 + (k % R::NK) * R::K_SLOT, vs = v_slot0 + (k % R::NV) * R::V_SLOT;
-        copies_wait<(R::NK < R::NV ? R::NK : R::NV) * 2 - 2>();
-        const uint4* wq = sh.attn + Shared::QF;
-        window_unit<BITS, MODE>(st, ks, vs, min(WIN_TOKENS, si.n_win - (win_first + k * win_stride) * WIN_TOKENS), [wq](int i) { return wq[i]; }, lane);
+        copies_wait<0>();
+        wide_window_unit<BITS, MODE>(st, k_slot0, min(WIDE_TOKENS, si.n_win - (win_first + k * win_stride) * WIDE_TOKENS), sh.attn + Shared::QF, lane);
         __syncwarp();
-        copy_rows(false, k + R::NK);
-        copy_rows(true, k + R::NV);
+        stage_window(k + 1);
     }
     copies_wait<0>();
-    if (score) { if (CL > 1) cluster.sync(); else __syncthreads(); }      // the list is complete
+    if (score && CL > 1) cluster.sync();                        // the list is complete
 
     // ---- the listed pages, 32 of this warp's at a time: lane k looks up the k-th
     const int wid = rank * SPARSE_WARPS + warp;
