@@ -241,7 +241,7 @@ struct SparseShared {
     float best[8][8];                     // per CTA of the cluster: largest score of its pages, per head
     int scan[SPARSE_WARPS], below[SPARSE_WARPS], equal[SPARSE_WARPS];
     unsigned most;                        // CTA 0: largest finite key
-    int bin, before, inside;              // CTA 0: the bin of the n_select-th key, keys in the bins ahead, keys in it
+    int bin, inside, wanted;              // CTA 0: the bin of the n_select-th key, keys in it, its rank among them
     unsigned kth;
     int n_list;
     unsigned list[SPARSE_THREADS];        // keys of that bin
@@ -311,7 +311,8 @@ __device__ __forceinline__ void wide_window_unit(WarpState<MODE>& st, unsigned r
 // with 16-byte asynchronous copies: a bulk copy costs the lane that requests it some 440 cycles, and requests of several lanes are
 // served one after the other (three per page and eight rows per window unit made the staging slower than the work on it).
 // Copies are waited for in the order of their groups: K_PENDING / V_PENDING groups may be outstanding behind the one that is needed
-// next, where the order is  K0 V0 [K1 [V1]]  then, per unit,  K(i + NK)  after its scores and  V(i + NV)  after its values.
+// next, where the order is  K0 V0  (K0 V0 K1 V1  with two slots each,  K0 K1 V0  with two and one), then, per unit,  K(i + NK)  after
+// its scores and  V(i + NV)  after its values.
 template <int BITS>
 struct Ring {
     static constexpr int NK = BITS == 4 ? 1 : 2, NV = BITS == 2 ? 2 : 1;
@@ -337,11 +338,11 @@ __device__ __forceinline__ int ld_early_s8(const signed char* p) {
     return v;
 }
 
-// Asynchronous copy of 16 bytes into shared memory; L2 drops the line first if `stream`.
+// Asynchronous copy of 16 bytes into shared memory, also with an L2 eviction policy.
 __device__ __forceinline__ void copy16(unsigned dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-__device__ __forceinline__ void copy16_stream(unsigned dst, const void* src, unsigned long long policy) {
+__device__ __forceinline__ void copy16_hint(unsigned dst, const void* src, unsigned long long policy) {
     asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -407,32 +408,22 @@ __device__ __forceinline__ void prefetch_bounds(const SparseParams& P, int page,
 // The n_select smallest of the keys (.x; .y is the page's id), ties to the lower page, in ascending order of the pages, by one CTA.
 // Keys are counted in bins of equal width; the bin of the n_select-th smallest is found by a prefix sum and its few keys are
 // compared with each other.
+// The code is kept short: a CTA runs through it once, so that every instruction is fetched for one use (with the keys in registers
+// and its loops unrolled it took 30 KB and was no faster).
 template <class Shared>
 __device__ __forceinline__ void list_pages(Shared& sh, const uint2* keys, int pages, int first, int n_select, int* out) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    constexpr unsigned INF_BITS = 0x7f800000u, NONE = 0xffffffffu;
-    // Every warp has a run of consecutive pages, 32 at a time; the first KEPT of its lanes' keys stay in registers.
-    constexpr int KEPT = 8;
-    const int run = (pages + SPARSE_THREADS - 1) / SPARSE_THREADS * 32, r_lo = min(warp * run, pages), r_hi = min(r_lo + run, pages);
-    unsigned mine[KEPT];
-#pragma unroll
-    for (int i = 0; i < KEPT; ++i) { const int p = r_lo + 32 * i + lane; mine[i] = p < r_hi ? keys[p].x : NONE; }
-    const auto each = [&](auto f) {                         // f(key) of all keys of this lane (and of places behind the run: NONE)
-#pragma unroll
-        for (int i = 0; i < KEPT; ++i) if (32 * i < run) f(mine[i]);
-        for (int p = r_lo + 32 * KEPT + lane; p < r_hi; p += 32) f(keys[p].x);
-    };
-    sh.bins[tid] = make_uint4(0u, 0u, 0u, 0u);
-    // bins of equal width from 0 to the largest key; the product is monotonic in the key, so bins are in the keys' order
+    // bins of equal width from 0 to the largest finite key; the product is monotonic in the key, so bins are in the keys' order
     const float width = __uint_as_float(sh.most), per_bin = width > 0.f ? (SELECT_BINS - 1) / width : 0.f;
-    const auto bin_of = [&](unsigned u) { return u < INF_BITS ? min(static_cast<int>(__uint_as_float(u) * per_bin), SELECT_BINS - 1) : SELECT_BINS - 1; };
+    const auto bin_of = [&](unsigned u) { return min(static_cast<int>(__uint_as_float(u) * per_bin), SELECT_BINS - 1); };
     unsigned* bins = reinterpret_cast<unsigned*>(sh.bins);
+    sh.bins[tid] = make_uint4(0u, 0u, 0u, 0u);
     __syncthreads();
-    each([&](unsigned u) { if (u != NONE) atomicAdd(bins + bin_of(u), 1u); });
+#pragma unroll 2
+    for (int p = tid; p < pages; p += SPARSE_THREADS) atomicAdd(bins + bin_of(keys[p].x), 1u);
     __syncthreads();
     const uint4 counted = sh.bins[tid];
-    const int counts[4] = {static_cast<int>(counted.x), static_cast<int>(counted.y), static_cast<int>(counted.z), static_cast<int>(counted.w)};
-    const int here = counts[0] + counts[1] + counts[2] + counts[3];
+    const int c0 = static_cast<int>(counted.x), c1 = static_cast<int>(counted.y), c2 = static_cast<int>(counted.z), here = c0 + c1 + c2 + static_cast<int>(counted.w);
     int before = here;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -444,23 +435,28 @@ __device__ __forceinline__ void list_pages(Shared& sh, const uint2* keys, int pa
     before -= here;
 #pragma unroll
     for (int w = 0; w < SPARSE_WARPS; ++w) before += w < warp ? sh.scan[w] : 0;
-    if (before < n_select && n_select <= before + here) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (before < n_select && n_select <= before + counts[e]) { sh.bin = 4 * tid + e; sh.before = before; sh.inside = counts[e]; }
-            before += counts[e];
-        }
+    const int rest = n_select - before;                     // the rank, from 1, of the n_select-th key among this thread's bins
+    if (rest >= 1 && rest <= here) {
+        const int e = (rest > c0) + (rest > c0 + c1) + (rest > c0 + c1 + c2);
+        const int skipped = e == 0 ? 0 : e == 1 ? c0 : e == 2 ? c0 + c1 : c0 + c1 + c2;
+        sh.bin = 4 * tid + e;
+        sh.wanted = rest - skipped - 1;
+        sh.inside = static_cast<int>(bins[4 * tid + e]);
     }
     __syncthreads();
-    const int bin = sh.bin, inside = sh.inside, wanted = n_select - sh.before - 1;      // rank of the n_select-th key in its bin
+    const int bin = sh.bin, inside = sh.inside, wanted = sh.wanted;      // the bin of the n_select-th key, keys in it, its rank there from 0
     unsigned kth = 0u;
     if (inside <= SPARSE_THREADS) {
-        each([&](unsigned u) { if (u != NONE && bin_of(u) == bin) sh.list[atomicAdd(&sh.n_list, 1)] = u; });
+#pragma unroll 2
+        for (int p = tid; p < pages; p += SPARSE_THREADS) {
+            const unsigned u = keys[p].x;
+            if (bin_of(u) == bin) sh.list[atomicAdd(&sh.n_list, 1)] = u;
+        }
         __syncthreads();
         if (tid < inside) {
             const unsigned u = sh.list[tid];
             int less = 0, same = 0;
-#pragma unroll 4
+#pragma unroll 2
             for (int k = 0; k < inside; ++k) { less += sh.list[k] < u; same += sh.list[k] == u; }
             if (less <= wanted && wanted < less + same) sh.kth = u;      // equal keys write the same
         }
@@ -468,12 +464,14 @@ __device__ __forceinline__ void list_pages(Shared& sh, const uint2* keys, int pa
         kth = sh.kth;
     } else {
         // many keys that are (almost) the same: bit by bit, the largest v with fewer than n_select keys below it
+#pragma unroll 1
         for (int bit = 30; bit >= 0; --bit) {
             const unsigned cand = kth | (1u << bit);
             int n = 0;
-            each([&](unsigned u) { n += u < cand; });
+#pragma unroll 1
+            for (int p = tid; p < pages; p += SPARSE_THREADS) n += keys[p].x < cand;
+            __syncthreads();                                // the readers of the round before
             n = __reduce_add_sync(FULL, n);
-            __syncthreads();
             if (lane == 0) sh.scan[warp] = n;
             __syncthreads();
             int total = 0;
@@ -482,9 +480,11 @@ __device__ __forceinline__ void list_pages(Shared& sh, const uint2* keys, int pa
             if (total < n_select) kth = cand;
         }
     }
-    // all below it, and of those equal to it the first ones
+    // all below it, and of those equal to it the first ones; every warp lists a run of consecutive pages
+    const int run = (pages + SPARSE_THREADS - 1) / SPARSE_THREADS * 32, r_lo = min(warp * run, pages), r_hi = min(r_lo + run, pages);
     int below = 0, equal = 0;
-    each([&](unsigned u) { below += u < kth; equal += u == kth; });
+#pragma unroll 2
+    for (int p = r_lo + lane; p < r_hi; p += 32) { const unsigned u = keys[p].x; below += u < kth; equal += u == kth; }
     below = __reduce_add_sync(FULL, below);
     equal = __reduce_add_sync(FULL, equal);
     if (lane == 0) { sh.below[warp] = below; sh.equal[warp] = equal; }
@@ -498,22 +498,20 @@ __device__ __forceinline__ void list_pages(Shared& sh, const uint2* keys, int pa
     }
     const int room = n_select - all_below;                  // places for keys equal to the n_select-th
     const unsigned lower = (1u << lane) - 1u;
-    int p = r_lo + lane;
-    const auto put = [&](unsigned u) {
-        const unsigned is_below = __ballot_sync(FULL, u < kth), is_equal = __ballot_sync(FULL, u == kth);
+#pragma unroll 1
+    for (int p0 = r_lo; p0 < r_hi; p0 += 32) {
+        const int p = p0 + lane;
+        const uint2 k = p < r_hi ? keys[p] : make_uint2(0xffffffffu, 0u);
+        const unsigned is_below = __ballot_sync(FULL, k.x < kth), is_equal = __ballot_sync(FULL, k.x == kth);
         const int e = equal_before + __popc(is_equal & lower);
-        if (u < kth || (u == kth && e < room)) {
+        if (k.x < kth || (k.x == kth && e < room)) {
             const int at = below_before + __popc(is_below & lower) + min(e, room);
             out[at] = first + p;
-            if (at < LISTED) sh.listed[at] = make_uint2(first + p, keys[p].y);
+            if (at < LISTED) sh.listed[at] = make_uint2(first + p, k.y);
         }
         below_before += __popc(is_below);
         equal_before += __popc(is_equal);
-        p += 32;
-    };
-#pragma unroll
-    for (int i = 0; i < KEPT; ++i) if (32 * i < run) put(mine[i]);
-    for (int i = KEPT; 32 * i < run; ++i) put(p < r_hi ? keys[p].x : NONE);
+    }
 }
 
 // One cluster of CL CTAs per (sequence, KV head).
@@ -610,7 +608,7 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
             const unsigned short* sink = c.sink_kv + plane * c.s_sink * D + piece * 8;
             const unsigned short* recent = c.ring_kv + plane * c.ring_cap * D + piece * 8;
             const int at0 = (si.recent_lo + max(w0 - si.n_sink, 0)) % c.ring_cap - max(w0, si.n_sink);      // ring row of window token w: at0 + w, or ring_cap less
-#pragma unroll
+#pragma unroll 2
             for (int j = 0; j < WIDE_TOKENS / 2; ++j) {
                 const int r = 2 * j + half, w = min(w0 + r, last);
                 const bool in_sink = w < si.n_sink;
@@ -841,17 +839,18 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
     for (int k = 0; k < NH; ++k) { const float2 v = sh.scal[MODE == 0 ? t : 2 * t + k]; fmul[k] = v.x; gadd[k] = v.y; }
     WarpState<MODE> st;
     st.reset();
-    const unsigned long long policy = l2_evict_first_policy();
+    unsigned long long policy;
+    if (P.stream_pages) policy = l2_evict_first_policy();
+    else asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
     // ---- window tokens
     if (score && CL == 1) __syncthreads();                      // the list is complete
-    if (P.ring_offset == 0) stage_window(0);
+#pragma unroll 1
     for (int k = 0; k < my_windows; ++k) {
+        if (k > 0 || P.ring_offset == 0) stage_window(k);
         copies_wait<0>();
         wide_window_unit<BITS, MODE>(st, k_slot0, min(WIDE_TOKENS, si.n_win - (win_first + k * win_stride) * WIDE_TOKENS), sh.attn + Shared::QF, lane);
         __syncwarp();
-        stage_window(k + 1);
     }
-    copies_wait<0>();
     if (score && CL > 1) cluster.sync();                        // the list is complete
 
     // ---- the listed pages, 32 of this warp's at a time: lane k looks up the k-th
@@ -873,15 +872,13 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
                 else atomicOr(c.dev_status, WUSHKV_DEV_BAD_PAGE_ID);
             }
         }
-        unsigned there = __ballot_sync(FULL, my_page >= 0), k_todo = there, v_todo = there;      // units of this warp, and those not yet requested
+        const unsigned all_there = __ballot_sync(FULL, my_page >= 0);
+        unsigned there = all_there, k_todo = there, v_todo = there;      // units of this warp, and those whose keys and values are not yet requested
         int ki = 0, vi = 0, k_slot = 0, v_slot = 0;             // slots of the next copies, of the unit at hand
         const auto copy_side = [&](unsigned dst, const unsigned char* src, int bytes) {
 #pragma unroll
             for (int i = 0; i < (bytes + 511) / 512; ++i)
-                if (bytes % 512 == 0 || 512 * i + 16 * lane < bytes) {
-                    if (P.stream_pages) copy16_stream(dst + 512 * i + 16 * lane, src + 512 * i + 16 * lane, policy);
-                    else copy16(dst + 512 * i + 16 * lane, src + 512 * i + 16 * lane);
-                }
+                if (bytes % 512 == 0 || 512 * i + 16 * lane < bytes) copy16_hint(dst + 512 * i + 16 * lane, src + 512 * i + 16 * lane, policy);
         };
         const auto copy_page = [&](bool value, unsigned& todo) {
             if (todo) {
@@ -899,48 +896,51 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
             }
             copies_commit();
         };
-        copy_page(false, k_todo);
-        copy_page(true, v_todo);
-        if (R::NK > 1) copy_page(false, k_todo);
-        if (R::NV > 1) copy_page(true, v_todo);
-        while (there) {
-            const int k = __ffs(there) - 1;
-            there &= there - 1;
-            const int pos0 = __shfl_sync(FULL, my_entry, k) * PAGE_TOKENS;
-            const unsigned ks = k_slot0 + k_slot * R::K_SLOT, vs = v_slot0 + v_slot * R::V_SLOT;
-            k_slot = k_slot + 1 == R::NK ? 0 : k_slot + 1;
-            v_slot = v_slot + 1 == R::NV ? 0 : v_slot + 1;
-            copies_wait<R::K_PENDING>();
+        // steps -2, -1 only request; every copy has one place in the code, which is executed once or twice per launch and fetched each time
+        constexpr int AHEAD = R::NK > R::NV ? R::NK : R::NV;
+#pragma unroll 1
+        for (int step = -AHEAD; step < __popc(all_there); ++step) {
             float sc[4][2 * NH];          // [block][row g: heads..., row g+8: heads...]
             unsigned vmeta[4][2];         // fp16x2 (Delta_v, x_min_v) of rows g, g+8
-            page_scores<BITS, MODE>(ks, ks + side_bytes(BITS), qf, qfl, gadd, sc, vmeta, lane);
-            __syncwarp();
-            copy_page(false, k_todo);                           // into the slot just read
-            if (pos0 < si.q_lo || pos0 + PAGE_TOKENS > si.q_hi) {      // first / last page of the quantized range: mask the tokens outside it
+            if (step >= 0) {
+                const int pos0 = __shfl_sync(FULL, my_entry, __ffs(there) - 1) * PAGE_TOKENS;
+                there &= there - 1;
+                const unsigned ks = k_slot0 + k_slot * R::K_SLOT;
+                k_slot = k_slot + 1 == R::NK ? 0 : k_slot + 1;
+                copies_wait<R::K_PENDING>();
+                page_scores<BITS, MODE>(ks, ks + side_bytes(BITS), qf, qfl, gadd, sc, vmeta, lane);
+                __syncwarp();
+                if (pos0 < si.q_lo || pos0 + PAGE_TOKENS > si.q_hi) {      // first / last page of the quantized range: mask the tokens outside it
 #pragma unroll
-                for (int bi = 0; bi < 4; ++bi)
+                    for (int bi = 0; bi < 4; ++bi)
 #pragma unroll
-                    for (int rs = 0; rs < 2; ++rs) {
-                        const int p = pos0 + bi * 16 + 8 * rs + g;
-                        if (p < si.q_lo || p >= si.q_hi) {
-                            vmeta[bi][rs] = 0u;
+                        for (int rs = 0; rs < 2; ++rs) {
+                            const int p = pos0 + bi * 16 + 8 * rs + g;
+                            if (p < si.q_lo || p >= si.q_hi) {
+                                vmeta[bi][rs] = 0u;
 #pragma unroll
-                            for (int j = 0; j < NH; ++j) sc[bi][rs * NH + j] = -INFINITY;
+                                for (int j = 0; j < NH; ++j) sc[bi][rs * NH + j] = -INFINITY;
+                            }
                         }
-                    }
+                }
             }
-            float mx[NH];
+            if (step >= -R::NK) copy_page(false, k_todo);       // into the slot just read
+            if (step >= 0) {
+                float mx[NH];
 #pragma unroll
-            for (int j = 0; j < NH; ++j) {
-                const float v = fmaxf(fmaxf(fmaxf(sc[0][j], sc[0][NH + j]), fmaxf(sc[1][j], sc[1][NH + j])),
-                                      fmaxf(fmaxf(sc[2][j], sc[2][NH + j]), fmaxf(sc[3][j], sc[3][NH + j])));
-                mx[j] = v * fmul[j];          // scores are kept divided by the head's multiplier (> 0)
+                for (int j = 0; j < NH; ++j) {
+                    const float v = fmaxf(fmaxf(fmaxf(sc[0][j], sc[0][NH + j]), fmaxf(sc[1][j], sc[1][NH + j])),
+                                          fmaxf(fmaxf(sc[2][j], sc[2][NH + j]), fmaxf(sc[3][j], sc[3][NH + j])));
+                    mx[j] = v * fmul[j];      // scores are kept divided by the head's multiplier (> 0)
+                }
+                st.raise_max(mx);
+                const unsigned vs = v_slot0 + v_slot * R::V_SLOT;
+                v_slot = v_slot + 1 == R::NV ? 0 : v_slot + 1;
+                copies_wait<R::V_PENDING>();
+                page_values<BITS, MODE>(st, vs, sc, vmeta, fmul, lane);
+                __syncwarp();
             }
-            st.raise_max(mx);
-            copies_wait<R::V_PENDING>();
-            page_values<BITS, MODE>(st, vs, sc, vmeta, fmul, lane);
-            __syncwarp();
-            copy_page(true, v_todo);
+            if (step >= -R::NV) copy_page(true, v_todo);
         }
         copies_wait<0>();
     }
