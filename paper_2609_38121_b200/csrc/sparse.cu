@@ -227,7 +227,7 @@ struct SparseShared {
     union {
         double q[GP][D];                  // the queries, in 64 bits
         uint4 frag[SETS * 4 * 32];        // then the selection's query fragments: [digit set][64 bytes of bounds][lane]
-        uint4 bins[SPARSE_THREADS];       // then, CTA 0: pages per bin of the range of keys
+        uint4 bins[SPARSE_THREADS];       // then this CTA's pages per bin of the range of keys
         float merged[GP][PART_STRIDE];    // at last the CTA's partial result of every head
     };
     union {
@@ -237,10 +237,9 @@ struct SparseShared {
     uint4 attn[QF + QW];                  // the attention's query fragments
     float2 scal[8];                       // score multiplier (log2 domain) and x_min multiplier of the heads
     float unit[8];                        // score of one unit of 2^e dot
-    float warp_best[SPARSE_WARPS][8];
-    float best[8][8];                     // per CTA of the cluster: largest score of its pages, per head
+    float2 warp_best[SPARSE_WARPS][8];
+    float2 best[8][8];                    // per CTA of the cluster: largest and smallest finite score of its pages, per head
     int scan[SPARSE_WARPS], below[SPARSE_WARPS], equal[SPARSE_WARPS];
-    unsigned most;                        // CTA 0: largest finite key
     int bin, inside, wanted;              // CTA 0: the bin of the n_select-th key, keys in it, its rank among them
     unsigned kth;
     int n_list;
@@ -405,24 +404,17 @@ __device__ __forceinline__ void prefetch_bounds(const SparseParams& P, int page,
     asm volatile("prefetch.global.L2 [%0];" ::"l"(P.exponents + ph));
 }
 
+// Bins of equal width; the product is monotonic in the key, so bins are in the keys' order.
+__device__ __forceinline__ int bin_of(unsigned key, float per_bin) { return min(static_cast<int>(__uint_as_float(key) * per_bin), SELECT_BINS - 1); }
+
 // The n_select smallest of the keys (.x; .y is the page's id), ties to the lower page, in ascending order of the pages, by one CTA.
-// Keys are counted in bins of equal width; the bin of the n_select-th smallest is found by a prefix sum and its few keys are
-// compared with each other.
+// counted: this thread's four of the bins of equal width in which the cluster has counted the keys; the bin of the n_select-th smallest
+// is found by a prefix sum and its few keys are compared with each other.
 // The code is kept short: a CTA runs through it once, so that every instruction is fetched for one use (with the keys in registers
 // and its loops unrolled it took 30 KB and was no faster).
 template <class Shared>
-__device__ __forceinline__ void list_pages(Shared& sh, const uint2* keys, int pages, int first, int n_select, int* out) {
+__device__ __forceinline__ void list_pages(Shared& sh, const uint4& counted, float per_bin, const uint2* keys, int pages, int first, int n_select, int* out) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    // bins of equal width from 0 to the largest finite key; the product is monotonic in the key, so bins are in the keys' order
-    const float width = __uint_as_float(sh.most), per_bin = width > 0.f ? (SELECT_BINS - 1) / width : 0.f;
-    const auto bin_of = [&](unsigned u) { return min(static_cast<int>(__uint_as_float(u) * per_bin), SELECT_BINS - 1); };
-    unsigned* bins = reinterpret_cast<unsigned*>(sh.bins);
-    sh.bins[tid] = make_uint4(0u, 0u, 0u, 0u);
-    __syncthreads();
-#pragma unroll 2
-    for (int p = tid; p < pages; p += SPARSE_THREADS) atomicAdd(bins + bin_of(keys[p].x), 1u);
-    __syncthreads();
-    const uint4 counted = sh.bins[tid];
     const int c0 = static_cast<int>(counted.x), c1 = static_cast<int>(counted.y), c2 = static_cast<int>(counted.z), here = c0 + c1 + c2 + static_cast<int>(counted.w);
     int before = here;
 #pragma unroll
@@ -441,7 +433,7 @@ __device__ __forceinline__ void list_pages(Shared& sh, const uint2* keys, int pa
         const int skipped = e == 0 ? 0 : e == 1 ? c0 : e == 2 ? c0 + c1 : c0 + c1 + c2;
         sh.bin = 4 * tid + e;
         sh.wanted = rest - skipped - 1;
-        sh.inside = static_cast<int>(bins[4 * tid + e]);
+        sh.inside = e == 0 ? c0 : e == 1 ? c1 : e == 2 ? c2 : here - c0 - c1 - c2;
     }
     __syncthreads();
     const int bin = sh.bin, inside = sh.inside, wanted = sh.wanted;      // the bin of the n_select-th key, keys in it, its rank there from 0
@@ -450,7 +442,7 @@ __device__ __forceinline__ void list_pages(Shared& sh, const uint2* keys, int pa
 #pragma unroll 2
         for (int p = tid; p < pages; p += SPARSE_THREADS) {
             const unsigned u = keys[p].x;
-            if (bin_of(u) == bin) sh.list[atomicAdd(&sh.n_list, 1)] = u;
+            if (bin_of(u, per_bin) == bin) sh.list[atomicAdd(&sh.n_list, 1)] = u;
         }
         __syncthreads();
         if (tid < inside) {
@@ -540,7 +532,7 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3, G = c.G;
     pdl_wait();
     pdl_launch_dependents();
-    if (tid == 0) { sh.most = 0u; sh.n_list = 0; }      // the other CTAs touch this one's shared memory after the first cluster barrier only
+    if (tid == 0) sh.n_list = 0;
     // ---- q': this thread's two rows of T_K^{-T} and its share of the queries are requested ahead of everything else
     constexpr int ROWS = D / CL, PAIRS = ROWS / 2, TPP = SPARSE_THREADS / PAIRS, QUADS = D / 4 / TPP;      // threads per pair of rows, float4 per thread and row
     constexpr int PART = QUADS > 4 ? 4 : QUADS;                                              // of them in flight together
@@ -745,9 +737,9 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
         uint4 bq[SETS][4];
 #pragma unroll
         for (int k = 0; k < SETS * 4; ++k) bq[k / 4][k % 4] = sh.frag[k * 32 + lane];
-        float unit[NH], best[NH];                               // heads per lane: t, or 2 t and 2 t + 1
+        float unit[NH], best[NH], worst[NH];                    // heads per lane: t, or 2 t and 2 t + 1
 #pragma unroll
-        for (int k = 0; k < NH; ++k) { const int head = MODE == 0 ? t : 2 * t + k; unit[k] = head < G ? sh.unit[head] : 0.f; best[k] = -INFINITY; }
+        for (int k = 0; k < NH; ++k) { const int head = MODE == 0 ? t : 2 * t + k; unit[k] = head < G ? sh.unit[head] : 0.f; best[k] = -INFINITY; worst[k] = INFINITY; }
         for (int p0 = 16 * warp; p0 < n_here; p0 += 16 * SPARSE_WARPS) {
             const BoundsTile now = tile;
             if (p0 + 16 * SPARSE_WARPS < n_here) tile.load(P, ids, h, p0 + 16 * SPARSE_WARPS, n_here, g, t);
@@ -773,53 +765,68 @@ __global__ void __launch_bounds__(SPARSE_THREADS, 2) sparse_decode_kernel(Sparse
                     const float s = now.good[rs] ? __fmul_rn(__int2float_rn(dot) * grid, unit[k]) : -INFINITY;
                     scores[head * per_max + p] = s;
                     best[k] = fmaxf(best[k], s);
+                    if (now.good[rs]) worst[k] = fminf(worst[k], s);
                 }
             }
         }
 #pragma unroll
         for (int k = 0; k < NH; ++k) {
-            best[k] = fmaxf(best[k], __shfl_xor_sync(FULL, best[k], 4));
-            best[k] = fmaxf(best[k], __shfl_xor_sync(FULL, best[k], 8));
-            best[k] = fmaxf(best[k], __shfl_xor_sync(FULL, best[k], 16));
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) {
+                best[k] = fmaxf(best[k], __shfl_xor_sync(FULL, best[k], o));
+                worst[k] = fminf(worst[k], __shfl_xor_sync(FULL, worst[k], o));
+            }
             const int head = MODE == 0 ? t : 2 * t + k;
-            if (g == 0) sh.warp_best[warp][head] = best[k];
+            if (g == 0) sh.warp_best[warp][head] = make_float2(best[k], worst[k]);
         }
         __syncthreads();
+        sh.bins[tid] = make_uint4(0u, 0u, 0u, 0u);              // in the place of the fragments, which every warp has read
         if (tid < 8 * CL) {
             const int head = tid & 7, peer = tid >> 3;
-            float m = -INFINITY;
+            float2 m = make_float2(-INFINITY, INFINITY);
             if (head < G)
 #pragma unroll
-                for (int w = 0; w < SPARSE_WARPS; ++w) m = fmaxf(m, sh.warp_best[w][head]);
-            float* to = CL > 1 ? cluster.map_shared_rank(&sh.best[0][0], peer) : &sh.best[0][0];
+                for (int w = 0; w < SPARSE_WARPS; ++w) { const float2 x = sh.warp_best[w][head]; m.x = fmaxf(m.x, x.x); m.y = fminf(m.y, x.y); }
+            float2* to = CL > 1 ? cluster.map_shared_rank(&sh.best[0][0], peer) : &sh.best[0][0];
             to[rank * 8 + head] = m;
         }
         if (CL > 1) cluster.sync(); else __syncthreads();
 
-        // ---- keys: bits of the distance below the best page (smaller is better)
+        // ---- keys: bits of the distance below the best page (smaller is better), counted in bins between 0 and the least range of a
+        // head's scores, which no finite key exceeds
         uint2* keys0 = CL > 1 ? cluster.map_shared_rank(keys, 0) : keys;
-        float top[GP];
+        float top[GP], width = INFINITY;
 #pragma unroll
         for (int j = 0; j < GP; ++j) {
-            float m = -INFINITY;
+            float2 m = make_float2(-INFINITY, INFINITY);
 #pragma unroll
-            for (int r = 0; r < CL; ++r) m = fmaxf(m, sh.best[r][j]);
-            top[j] = m == -INFINITY ? 0.f : m;
+            for (int r = 0; r < CL; ++r) { const float2 x = sh.best[r][j]; m.x = fmaxf(m.x, x.x); m.y = fminf(m.y, x.y); }
+            top[j] = m.x == -INFINITY ? 0.f : m.x;
+            if (j < G) width = fminf(width, m.x - m.y);
         }
-        unsigned most = 0u;
+        const float per_bin = width > 0.f && width < INFINITY ? (SELECT_BINS - 1) / width : 0.f;
         for (int p = tid; p < n_here; p += SPARSE_THREADS) {
             float key = -INFINITY;
 #pragma unroll
             for (int j = 0; j < GP; ++j) if (j < G) key = fmaxf(key, __fsub_rn(scores[j * per_max + p], top[j]));
             const unsigned u = __float_as_uint(key) & 0x7fffffffu;
             keys0[p_lo + p] = make_uint2(u, static_cast<unsigned>(ids[p]));
-            if (u < 0x7f800000u) most = max(most, u);
+            atomicAdd(reinterpret_cast<unsigned*>(sh.bins) + bin_of(u, per_bin), 1u);
         }
-        most = __reduce_max_sync(FULL, most);
-        if (lane == 0 && most > 0u) atomicMax(CL > 1 ? cluster.map_shared_rank(&sh.most, 0) : &sh.most, most);
         if (CL > 1) cluster.sync(); else __syncthreads();
-        if (rank == 0) list_pages(sh, keys, pages, first, P.n_select, list);
-        if (!attend) return;
+        if (rank == 0) {
+            uint4 counted = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int r = 0; r < CL; ++r) {
+                const uint4 x = *(CL > 1 ? cluster.map_shared_rank(&sh.bins[tid], r) : &sh.bins[tid]);
+                counted.x += x.x; counted.y += x.y; counted.z += x.z; counted.w += x.w;
+            }
+            list_pages(sh, counted, per_bin, keys, pages, first, P.n_select, list);
+        }
+        if (!attend) {
+            if (CL > 1) cluster.sync();                         // no CTA leaves while its bins are read
+            return;
+        }
         if (CL > 1 && rank == 0) __syncthreads();               // the keys' place may become the staging ring
     }
 
