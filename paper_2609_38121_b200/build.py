@@ -15,7 +15,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "build")
 LIB = os.path.join(HERE, "libwushkv.so")
-SOURCES = ["api.cu", "transforms_host.cpp", "append.cu", "decode.cu", "decode_static.cu", "prefill.cu", "calibrate.cu", "hessians.cu", "sparse.cu", "page_pool.cu"]
+SOURCES = ["api.cu", "transforms_host.cpp", "append.cu", "decode.cu", "decode_static.cu", "prefill.cu", "calibrate.cu", "hessians.cu", "sparse.cu",
+           "sparse_2bit.cu", "sparse_3bit.cu", "sparse_4bit.cu", "page_pool.cu"]
 ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
 
 
