@@ -40,36 +40,29 @@ __device__ __forceinline__ void halve(float* v, int lane, int bit) {
     }
 }
 
-// Two numbers per instruction, and minima and maxima of three.
-__device__ __forceinline__ unsigned long long pack2(float a, float b) {
-    unsigned long long d;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
-    return d;
-}
-__device__ __forceinline__ void unpack2(unsigned long long d, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(d)); }
-__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
-    unsigned long long d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
-    unsigned long long d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
+// Minima and maxima of three; a * b + c of two halves and a float, rounded once.
 __device__ __forceinline__ float min3(float a, float b, float c) { float d; asm("min.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
 __device__ __forceinline__ float max3(float a, float b, float c) { float d; asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
+__device__ __forceinline__ float fma_half(unsigned short a, unsigned short b, float c) {
+    float d;
+    asm("fma.rn.f32.f16 %0, %1, %2, %3;" : "=f"(d) : "h"(a), "h"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ void halves(unsigned w, unsigned short& lo, unsigned short& hi) { asm("mov.b32 {%0, %1}, %2;" : "=h"(lo), "=h"(hi) : "r"(w)); }
 
 // A warp per (page, head).  Lane (g, t) reads the code words of token rows g and g + 8 of every 16-token block, which hold the
 // channels 32 s + 16 hh + 8 u + 2 t + v of all s, hh, u, v: 32 running minima and maxima per lane, combined over g at the end.
-// What bounds it is instructions (256 codes per lane): a code becomes a float by a byte permute that puts its byte, masked to one
-// field, under the exponent of 2^23, the rest is done for the two token rows at once.
+// What bounds it is the integer pipe (256 codes per lane).  A code masked out of a 16-bit half at bit F is, read as fp16, the number
+// code * 2^(F - 24); one multiply-add of halves gives 2^(F - 24) khat from it and the stored step, so that a code costs half a mask,
+// one multiply-add and a half each of a three-input minimum and maximum.  8 x 8192 tokens of 4 heads at 2 bits: 11.1 us with the codes
+// turned into floats by byte permutes (2.25 integer instructions per code instead of 1.6).
+constexpr int BOUNDS_WARPS = 2;      // per CTA: few, so that the last wave of CTAs is short
 template <int BITS>
-__global__ void __launch_bounds__(256) page_bounds_kernel(BoundsParams P) {
+__global__ void __launch_bounds__(BOUNDS_WARPS * 32) page_bounds_kernel(BoundsParams P) {
     constexpr int REC = record_bytes(BITS), CB = code_block_bytes(BITS);
     const CacheView& c = P.c;
     const int b = blockIdx.y, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int unit = blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int unit = blockIdx.x * BOUNDS_WARPS + (threadIdx.x >> 5);
     const int len = P.seq_len[b], n = P.cu_new[b + 1] - P.cu_new[b], slot = P.slot[b];
     if (n <= 0 || len <= 0) return;
     if (slot < 0 || slot >= c.n_slots) { if (unit == 0 && lane == 0) atomicOr(c.dev_status, WUSHKV_DEV_BAD_SLOT); return; }
@@ -90,58 +83,61 @@ __global__ void __launch_bounds__(256) page_bounds_kernel(BoundsParams P) {
         if (BITS == 3) high[bi] = __ldg(reinterpret_cast<const uint2*>(rec + k_hi_offset(3) + bi * 256) + lane);
         meta[bi] = __ldg(reinterpret_cast<const uint4*>(rec + meta_offset(BITS) + 128 * bi) + g);
     }
-    constexpr float MAGIC = 8388608.f;                       // 2^23
-    const unsigned long long unmagic = pack2(-MAGIC, -MAGIC);
     float lo[32], hi[32];
 #pragma unroll
     for (int j = 0; j < 32; ++j) { lo[j] = INFINITY; hi[j] = -INFINITY; }
 #pragma unroll
     for (int bi = 0; bi < 4; ++bi) {
-        float step[2], low[2];
+        unsigned short step[2];
+        float low[2];
 #pragma unroll
         for (int rs = 0; rs < 2; ++rs) {
-            const unsigned m = rs == 0 ? meta[bi].x : meta[bi].z;
-            __half2 h2;
-            *reinterpret_cast<unsigned*>(&h2) = m;
-            const float2 f = __half22float2(h2);
-            const bool there = index * PAGE_TOKENS + 16 * bi + 8 * rs + g < len;
-            step[rs] = there ? f.x : 0.f;
-            low[rs] = there ? f.y : NAN;                 // minimum and maximum pass over a NaN: a token that is not there, or a damaged one
+            unsigned short offset;
+            halves(rs == 0 ? meta[bi].x : meta[bi].z, step[rs], offset);
+            // minimum and maximum pass over a NaN: a token that is not there, or a damaged one
+            low[rs] = index * PAGE_TOKENS + 16 * bi + 8 * rs + g < len ? __half2float(__ushort_as_half(offset)) : NAN;
         }
-        const unsigned long long low2 = pack2(low[0], low[1]);
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            // a code in bits F .. of its byte is code * 2^F; the step takes the 2^-F, both exact
-            constexpr unsigned FIELD = BITS == 4 ? 0x0F0F0F0Fu : 0x03030303u;
-            const int shift = BITS == 4 ? 4 * (s & 1) : 2 * s;
-            const float down = 1.f / static_cast<float>(1 << shift);
-            const unsigned long long step2 = pack2(step[0] * down, step[1] * down);
+            const int at = BITS == 4 ? 4 * (s & 1) : 2 * s;               // bit of the field in its byte
+            const float unit = 1.f / static_cast<float>(1 << (24 - at));
+            const float low_unit[2] = {low[0] * unit, low[1] * unit};
 #pragma unroll
             for (int hh = 0; hh < 2; ++hh) {
                 const uint4& q = words[bi][BITS == 4 ? s >> 1 : 0];
-                unsigned w[2] = {hh == 0 ? q.x : q.z, hh == 0 ? q.y : q.w};
 #pragma unroll
-                for (int rs = 0; rs < 2; ++rs) {
-                    w[rs] &= FIELD << shift;
-                    if (BITS == 3) {
-                        // the third bit, 4 * 2^F: for the uppermost field it would leave its byte, so that one is moved down
-                        const unsigned hb = ((rs == 0 ? high[bi].x : high[bi].y) >> (2 * s + hh)) & 0x01010101u;
-                        w[rs] = s < 3 ? w[rs] | (hb << (shift + 2)) : (w[rs] >> 2) | (hb << 6);
+                for (int odd = 0; odd < 2; ++odd) {                        // bytes 0 and 2, or 1 and 3 of the words
+                    float v[2][2];                                         // [byte][row half]
+#pragma unroll
+                    for (int rs = 0; rs < 2; ++rs) {
+                        const unsigned w = (hh == 0 ? (rs == 0 ? q.x : q.y) : (rs == 0 ? q.z : q.w)) >> (8 * odd);
+                        unsigned code = w & ((BITS == 4 ? 0x000F000Fu : 0x00030003u) << at);
+                        if (BITS == 3) {
+                            const unsigned hw = rs == 0 ? high[bi].x : high[bi].y;
+                            const int shift = at + 2 - (8 * odd + 2 * s + hh);     // the third bit: from bit 2 s + hh of its byte to two above the field
+                            code |= (shift >= 0 ? hw << shift : hw >> -shift) & (0x00010001u << (at + 2));
+                        }
+                        unsigned short c0, c1;
+                        halves(code, c0, c1);
+                        // the product has at most 15 bits: the multiply-add rounds once, as the sum alone does
+                        v[0][rs] = fma_half(c0, step[rs], low_unit[rs]);
+                        v[1][rs] = fma_half(c1, step[rs], low_unit[rs]);
                     }
-                }
-                const unsigned long long step_here = BITS == 3 && s == 3 ? pack2(step[0] * (1.f / 16.f), step[1] * (1.f / 16.f)) : step2;
 #pragma unroll
-                for (int by = 0; by < 4; ++by) {
-                    const float x0 = __uint_as_float(__byte_perm(w[0], 0x4B000000u, 0x7440u + by)), x1 = __uint_as_float(__byte_perm(w[1], 0x4B000000u, 0x7440u + by));
-                    // step * code has at most 15 bits: the multiply-add rounds once, as the sum alone does
-                    float v0, v1;
-                    unpack2(fma2(step_here, add2(pack2(x0, x1), unmagic), low2), v0, v1);
-                    const int j = 8 * s + 4 * hh + by;
-                    lo[j] = min3(lo[j], v0, v1);
-                    hi[j] = max3(hi[j], v0, v1);
+                    for (int k = 0; k < 2; ++k) {
+                        const int j = 8 * s + 4 * hh + 2 * k + odd;
+                        lo[j] = min3(lo[j], v[k][0], v[k][1]);
+                        hi[j] = max3(hi[j], v[k][0], v[k][1]);
+                    }
                 }
             }
         }
+    }
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+        const float up = static_cast<float>(1 << (24 - (BITS == 4 ? 4 * ((j >> 3) & 1) : 2 * (j >> 3))));
+        lo[j] *= up;
+        hi[j] *= up;
     }
     halve<16, false>(lo, lane, 16); halve<16, true>(hi, lane, 16);
     halve<8, false>(lo, lane, 8);   halve<8, true>(hi, lane, 8);
@@ -217,11 +213,11 @@ extern "C" int wushkv_update_page_bounds(const wushkv_cache* cache, int32_t batc
     if (max_new == 0) return WUSHKV_OK;
     P.slot = slot; P.seq_len = seq_len; P.cu_new = cu_new; P.bounds = bounds; P.exponents = exponents;
     const long long pages = (static_cast<long long>(max_new) + PAGE_TOKENS - 2) / PAGE_TOKENS + 1;       // that max_new consecutive tokens can touch
-    const dim3 grid(static_cast<unsigned>((pages * P.c.n_kv + 7) / 8), batch);
+    const dim3 grid(static_cast<unsigned>((pages * P.c.n_kv + BOUNDS_WARPS - 1) / BOUNDS_WARPS), batch);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (P.c.bits == 2) page_bounds_kernel<2><<<grid, 256, 0, st>>>(P);
-    else if (P.c.bits == 3) page_bounds_kernel<3><<<grid, 256, 0, st>>>(P);
-    else page_bounds_kernel<4><<<grid, 256, 0, st>>>(P);
+    if (P.c.bits == 2) page_bounds_kernel<2><<<grid, BOUNDS_WARPS * 32, 0, st>>>(P);
+    else if (P.c.bits == 3) page_bounds_kernel<3><<<grid, BOUNDS_WARPS * 32, 0, st>>>(P);
+    else page_bounds_kernel<4><<<grid, BOUNDS_WARPS * 32, 0, st>>>(P);
     return cudaPeekAtLastError() == cudaSuccess ? WUSHKV_OK : WUSHKV_ECUDA;
 }
 
