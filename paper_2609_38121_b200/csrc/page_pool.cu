@@ -8,8 +8,9 @@
 //
 // reserve and compact need ranks over the whole pool (the k-th free page).  They run as ONE cluster of eight CTAs: every CTA
 // counts its eighth of the pool, the counts meet at a cluster barrier, and a second walk writes each page's rank, so that a
-// pool of some ten thousand pages takes one launch of a few microseconds.  What bounds them is latency (the barriers and the
-// dependent loads table entry -> count), not the 4 bytes per page and entry that they read.
+// call is one launch.  What bounds them is latency (the barriers and the dependent loads table entry -> count), not the 4 bytes
+// per page and entry that they read; one CTA of 1024 threads, without cluster barriers, took 14.0 us instead of 7.9 to compact
+// 5600 pages of 64 sequences, and 9.8 instead of 8.1 us to reserve 12.
 //
 // The copies move whole records with 16-byte loads and stores, a warp per record with all of its loads in flight; they are
 // bound by HBM.
@@ -53,6 +54,8 @@ __device__ __forceinline__ void drop_page(const PoolView& v, int entry) {
 // A CTA per sequence, a thread per table entry.  Entries are exchanged, not overwritten, so that the counts stay right even
 // when a row is named twice in a call.
 __global__ void __launch_bounds__(256) pages_fork_kernel(PoolView v, const int* src_slot, const int* dst_slot, const int* src_len) {
+    pdl_wait();
+    pdl_launch_dependents();
     const int k = blockIdx.x;
     const int src = src_slot[k], dst = dst_slot[k], len = src_len[k];
     if (src < 0 || src >= v.n_slots || dst < 0 || dst >= v.n_slots) {
@@ -78,6 +81,8 @@ __global__ void __launch_bounds__(256) pages_fork_kernel(PoolView v, const int* 
 }
 
 __global__ void __launch_bounds__(256) pages_release_kernel(PoolView v, const int* slot, const int* keep_len) {
+    pdl_wait();
+    pdl_launch_dependents();
     const int k = blockIdx.x, s = slot[k];
     if (s < 0 || s >= v.n_slots) {
         if (threadIdx.x == 0) atomicOr(v.dev_status, WUSHKV_DEV_BAD_SLOT);
@@ -161,9 +166,11 @@ __device__ __forceinline__ bool request_of(const ReserveParams& P, int b, Reques
 }
 
 __global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS) pages_reserve_kernel(ReserveParams P) {
+    pdl_wait();
+    pdl_launch_dependents();
     cg::cluster_group cluster = cg::this_cluster();
     const PoolView& v = P.v;
-    const int rank = static_cast<int>(cluster.block_rank()), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int rank = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     __shared__ int scratch[POOL_WARPS];
     __shared__ int tile[POOL_THREADS];
     __shared__ int free_s, total_s, copies_s;            // free pages of this CTA's part; CTA 0: pages and copies asked for
@@ -304,7 +311,7 @@ __global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS
         *P.n_copies = written;
         if (!granted) atomicOr(v.dev_status, WUSHKV_DEV_POOL_EMPTY);
     }
-    cluster.sync();                                      // no CTA leaves while another reads its counts
+    cluster.sync();                                   // no CTA leaves while another reads its counts
 }
 
 // ---- compact ---------------------------------------------------------------------------------------------------------------
@@ -321,9 +328,11 @@ struct CompactParams {
 };
 
 __global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS) pages_compact_kernel(CompactParams P) {
+    pdl_wait();
+    pdl_launch_dependents();
     cg::cluster_group cluster = cg::this_cluster();
     const PoolView& v = P.v;
-    const int rank = static_cast<int>(cluster.block_rank());
+    const int rank = blockIdx.x;
     __shared__ int scratch[POOL_WARPS];
     __shared__ int live_s, holes_s;
     int lo, hi;
@@ -408,6 +417,8 @@ struct CopyPagesParams {
 
 template <int BITS>
 __global__ void __launch_bounds__(256) copy_pages_kernel(CopyPagesParams P) {
+    pdl_wait();
+    pdl_launch_dependents();
     constexpr int REC = record_bytes(BITS), VECS = REC / 16, PER_LANE = (VECS + 31) / 32;
     static_assert(REC % 16 == 0, "records are copied in 16-byte vectors");
     const int lane = threadIdx.x & 31;
@@ -454,6 +465,8 @@ constexpr int WINDOW_VECS = 8;                           // 16-byte vectors per 
 
 // blockIdx.y: the copy; its rows are numbered (plane, sink rows then ring rows), 16 vectors each.
 __global__ void __launch_bounds__(256) copy_windows_kernel(CopyWindowsParams P) {
+    pdl_wait();
+    pdl_launch_dependents();
     const int k = blockIdx.y, src = P.src_slot[k], dst = P.dst_slot[k], len = P.src_len[k];
     if (src < 0 || src >= P.n_slots || dst < 0 || dst >= P.n_slots) {
         if (threadIdx.x == 0 && blockIdx.x == 0) atomicOr(P.dev_status, WUSHKV_DEV_BAD_SLOT);
@@ -499,7 +512,7 @@ static size_t pool_workspace_ints(const PoolView& v, int batch) {
     return std::max(reserve, 3 * static_cast<size_t>(v.n_pages));
 }
 
-static int launched() { return cudaPeekAtLastError() == cudaSuccess ? WUSHKV_OK : WUSHKV_ECUDA; }
+static int launched(cudaError_t e) { return e == cudaSuccess ? WUSHKV_OK : WUSHKV_ECUDA; }
 
 }  // namespace wushkv
 
@@ -523,8 +536,7 @@ extern "C" int wushkv_pages_reserve(const wushkv_page_pool* pool, int32_t batch,
     P.need = static_cast<int*>(workspace);
     P.shared = P.need + batch;
     P.list = P.shared + batch;
-    pages_reserve_kernel<<<POOL_CTAS, POOL_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(P);
-    return launched();
+    return launched(launch_pdl(pages_reserve_kernel, dim3(POOL_CTAS), dim3(POOL_THREADS), 0, static_cast<cudaStream_t>(stream), P));
 }
 
 extern "C" int wushkv_pages_fork(const wushkv_page_pool* pool, int32_t n, const int32_t* src_slot, const int32_t* dst_slot, const int32_t* src_len, void* stream) {
@@ -533,8 +545,7 @@ extern "C" int wushkv_pages_fork(const wushkv_page_pool* pool, int32_t n, const 
     if (rc != WUSHKV_OK) return rc;
     if (n < 0 || !src_slot || !dst_slot || !src_len) return WUSHKV_EINVAL;
     if (n == 0) return WUSHKV_OK;
-    pages_fork_kernel<<<n, 256, 0, static_cast<cudaStream_t>(stream)>>>(v, src_slot, dst_slot, src_len);
-    return launched();
+    return launched(launch_pdl(pages_fork_kernel, dim3(n), dim3(256), 0, static_cast<cudaStream_t>(stream), v, src_slot, dst_slot, src_len));
 }
 
 extern "C" int wushkv_pages_release(const wushkv_page_pool* pool, int32_t n, const int32_t* slot, const int32_t* keep_len, void* stream) {
@@ -543,8 +554,7 @@ extern "C" int wushkv_pages_release(const wushkv_page_pool* pool, int32_t n, con
     if (rc != WUSHKV_OK) return rc;
     if (n < 0 || !slot) return WUSHKV_EINVAL;
     if (n == 0) return WUSHKV_OK;
-    pages_release_kernel<<<n, 256, 0, static_cast<cudaStream_t>(stream)>>>(v, slot, keep_len);
-    return launched();
+    return launched(launch_pdl(pages_release_kernel, dim3(n), dim3(256), 0, static_cast<cudaStream_t>(stream), v, slot, keep_len));
 }
 
 extern "C" int wushkv_pages_compact(const wushkv_page_pool* pool, int32_t* copy_src, int32_t* copy_dst, int32_t* n_copies, int32_t* n_live,
@@ -559,8 +569,7 @@ extern "C" int wushkv_pages_compact(const wushkv_page_pool* pool, int32_t* copy_
     P.movers = P.holes + P.v.n_pages;
     P.moved = P.movers + P.v.n_pages;
     P.n_list = (P.v.n_pages + 1) / 2;
-    pages_compact_kernel<<<POOL_CTAS, POOL_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(P);
-    return launched();
+    return launched(launch_pdl(pages_compact_kernel, dim3(POOL_CTAS), dim3(POOL_THREADS), 0, static_cast<cudaStream_t>(stream), P));
 }
 
 extern "C" int wushkv_copy_pages(const wushkv_cache* cache, int32_t max_copies, const int32_t* copy_src, const int32_t* copy_dst, const int32_t* n_copies,
@@ -577,10 +586,7 @@ extern "C" int wushkv_copy_pages(const wushkv_cache* cache, int32_t max_copies, 
     const long long ctas = std::min<long long>((static_cast<long long>(max_copies) * c.n_kv + 7) / 8, 6ll * sm_count());
     const dim3 grid(static_cast<unsigned>(ctas));
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (c.bits == 2) copy_pages_kernel<2><<<grid, 256, 0, st>>>(P);
-    else if (c.bits == 3) copy_pages_kernel<3><<<grid, 256, 0, st>>>(P);
-    else copy_pages_kernel<4><<<grid, 256, 0, st>>>(P);
-    return launched();
+    return launched(launch_pdl(c.bits == 2 ? copy_pages_kernel<2> : c.bits == 3 ? copy_pages_kernel<3> : copy_pages_kernel<4>, grid, dim3(256), 0, st, P));
 }
 
 extern "C" int wushkv_copy_windows(const wushkv_cache* cache, int32_t n, const int32_t* src_slot, const int32_t* dst_slot, const int32_t* src_len, void* stream) {
@@ -595,6 +601,5 @@ extern "C" int wushkv_copy_windows(const wushkv_cache* cache, int32_t n, const i
     P.n_slots = c.n_slots; P.planes = 2 * c.n_kv; P.s_sink = c.s_sink; P.ring_cap = c.ring_cap;
     const long long vecs = static_cast<long long>(P.planes) * (P.s_sink + P.ring_cap) * (D / 8);
     const dim3 grid(static_cast<unsigned>((vecs + 256 * WINDOW_VECS - 1) / (256 * WINDOW_VECS)), n);
-    copy_windows_kernel<<<grid, 256, 0, static_cast<cudaStream_t>(stream)>>>(P);
-    return launched();
+    return launched(launch_pdl(copy_windows_kernel, grid, dim3(256), 0, static_cast<cudaStream_t>(stream), P));
 }

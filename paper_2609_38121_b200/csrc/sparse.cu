@@ -60,6 +60,8 @@ constexpr int BOUNDS_WARPS = 2;      // per CTA: few, so that the last wave of C
 template <int BITS>
 __global__ void __launch_bounds__(BOUNDS_WARPS * 32) page_bounds_kernel(BoundsParams P) {
     constexpr int REC = record_bytes(BITS), CB = code_block_bytes(BITS);
+    pdl_wait();
+    pdl_launch_dependents();
     const CacheView& c = P.c;
     const int b = blockIdx.y, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int unit = blockIdx.x * BOUNDS_WARPS + (threadIdx.x >> 5);
@@ -79,9 +81,9 @@ __global__ void __launch_bounds__(BOUNDS_WARPS * 32) page_bounds_kernel(BoundsPa
 #pragma unroll
     for (int bi = 0; bi < 4; ++bi) {
 #pragma unroll
-        for (int p = 0; p < (BITS == 4 ? 2 : 1); ++p) words[bi][p] = __ldg(reinterpret_cast<const uint4*>(rec + bi * CB + 512 * p) + lane);
-        if (BITS == 3) high[bi] = __ldg(reinterpret_cast<const uint2*>(rec + k_hi_offset(3) + bi * 256) + lane);
-        meta[bi] = __ldg(reinterpret_cast<const uint4*>(rec + meta_offset(BITS) + 128 * bi) + g);
+        for (int p = 0; p < (BITS == 4 ? 2 : 1); ++p) words[bi][p] = ld_in(reinterpret_cast<const uint4*>(rec + bi * CB + 512 * p) + lane);
+        if (BITS == 3) high[bi] = ld_in(reinterpret_cast<const uint2*>(rec + k_hi_offset(3) + bi * 256) + lane);
+        meta[bi] = ld_in(reinterpret_cast<const uint4*>(rec + meta_offset(BITS) + 128 * bi) + g);
     }
     float lo[32], hi[32];
 #pragma unroll
@@ -215,12 +217,9 @@ extern "C" int wushkv_update_page_bounds(const wushkv_cache* cache, int32_t batc
     const long long pages = (static_cast<long long>(max_new) + PAGE_TOKENS - 2) / PAGE_TOKENS + 1;       // that max_new consecutive tokens can touch
     const dim3 grid(static_cast<unsigned>((pages * P.c.n_kv + BOUNDS_WARPS - 1) / BOUNDS_WARPS), batch);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (P.c.bits == 2) page_bounds_kernel<2><<<grid, BOUNDS_WARPS * 32, 0, st>>>(P);
-    else if (P.c.bits == 3) page_bounds_kernel<3><<<grid, BOUNDS_WARPS * 32, 0, st>>>(P);
-    else page_bounds_kernel<4><<<grid, BOUNDS_WARPS * 32, 0, st>>>(P);
-    return cudaPeekAtLastError() == cudaSuccess ? WUSHKV_OK : WUSHKV_ECUDA;
+    return launch_pdl(P.c.bits == 2 ? page_bounds_kernel<2> : P.c.bits == 3 ? page_bounds_kernel<3> : page_bounds_kernel<4>, grid, dim3(BOUNDS_WARPS * 32), 0, st, P) == cudaSuccess
+        ? WUSHKV_OK : WUSHKV_ECUDA;
 }
-
 extern "C" int wushkv_select_pages(const wushkv_cache* cache, int32_t batch, const int32_t* slot, const int32_t* seq_len, int32_t max_seq_len,
                                    const uint16_t* Q, const wushkv_prologue* prologue, const int8_t* bounds, const int8_t* exponents,
                                    int32_t n_select, int32_t* selected, void* stream) {

@@ -147,15 +147,16 @@ struct Ring {
 
 __host__ __device__ inline int pages_per_cta(int pages, int cl) { return ((pages + cl - 1) / cl + 15) / 16 * 16; }
 
-// Loads that stay where they are written: ahead of the work that their latency is to hide behind.
+// Loads that stay where they are written: behind pdl_wait() (what they read may come from the kernel ahead, so they do not take the
+// read-only path either) and ahead of the work that their latency is to hide behind.
 __device__ __forceinline__ uint4 ld_early(const uint4* p) {
     uint4 v;
-    asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
 __device__ __forceinline__ int ld_early_s8(const signed char* p) {
     int v;
-    asm volatile("ld.global.nc.s8 %0, [%1];" : "=r"(v) : "l"(p));
+    asm volatile("ld.global.s8 %0, [%1];" : "=r"(v) : "l"(p));
     return v;
 }
 
@@ -371,7 +372,7 @@ __global__ void __launch_bounds__(NT, 2) sparse_decode_kernel(SparseParams P) {
     };
     load_T(0);
     uint2 q_bits = make_uint2(0u, 0u);                  // slots without a head are zero
-    if (warp < G) q_bits = __ldg(reinterpret_cast<const uint2*>(P.Q + (static_cast<long long>(b) * c.n_q + h * G + warp) * D + 4 * lane));
+    if (warp < G) q_bits = ld_in(reinterpret_cast<const uint2*>(P.Q + (static_cast<long long>(b) * c.n_q + h * G + warp) * D + 4 * lane));
 
     // ---- candidates
     const int S = __ldcg(P.seq_len + b), slot = P.slot[b];
@@ -403,7 +404,7 @@ __global__ void __launch_bounds__(NT, 2) sparse_decode_kernel(SparseParams P) {
     const int* row = c.page_table + static_cast<long long>(slot) * c.max_pages;              // read only if there are pages
     if (score) {
         for (int p = tid; p < n_here; p += NT) {
-            const int page = __ldg(row + first + p_lo + p);
+            const int page = ld_in(row + first + p_lo + p);
             const bool good = page >= 0 && page < c.n_pages;
             if (good) prefetch_bounds(P, page, h);
             else atomicOr(c.dev_status, WUSHKV_DEV_BAD_PAGE_ID);
@@ -719,7 +720,7 @@ __global__ void __launch_bounds__(NT, 2) sparse_decode_kernel(SparseParams P) {
                 my_page = static_cast<int>(e.y);                // -1: flagged when it was scored
             } else if ((my_entry = given || score ? __ldcg(list + u) : first + u) != -1) {
                 const bool inside = my_entry >= first && my_entry < first + pages;
-                const int page = inside ? __ldg(row + my_entry) : -1;
+                const int page = inside ? ld_in(row + my_entry) : -1;
                 if (page >= 0 && page < c.n_pages) my_page = page;
                 else atomicOr(c.dev_status, WUSHKV_DEV_BAD_PAGE_ID);
             }
