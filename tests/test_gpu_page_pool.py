@@ -171,6 +171,10 @@ def test_bad_slots_pages_and_counts_are_flagged():
     assert flagged(0) and p.torch.equal(p.gpu.page_table[1], before[0][1])
     p.gpu.release(1, p.ints([2]))
     assert flagged(0) and same()
+    p.gpu.reserve([], 1, p.ints([2]), p.ints([40]), p.ints([0, 1]))              # a partly filled page that is not there: its tokens are lost
+    assert flagged(B.DEV_BAD_PAGE_ID) and int(p.gpu.page_table[2, 0]) >= 0 and int(p.gpu.n_copies.item()) == 0
+    p.gpu.release(1, p.ints([2]))
+    assert flagged(0) and same()
     p.gpu.page_table[2, 0] = 20                                                  # no page of the pool
     p.gpu.release(1, p.ints([2]))
     assert flagged(B.DEV_BAD_PAGE_ID) and same()

@@ -195,6 +195,26 @@ def test_more_pages_than_a_warp_step_and_many_sequences():
     s.check(17)
 
 
+def test_more_heads_than_the_gpu_holds_at_once():
+    """512 (sequence, KV head) pairs in several waves; some of them against the oracle, all of them finite; rows behind the batch stay."""
+    lengths = [140 + (61 * i) % 500 for i in range(64)]
+    s = Sparse(lengths, 32, 8, 4, seed=24)
+    q, Q = s.queries()
+    sel = s.torch.full((66, 8, 3), -9, dtype=s.torch.int32, device="cuda")
+    out = s.torch.full((66, 32, 128), 7.0, dtype=s.torch.bfloat16, device="cuda")
+    s.B.decode_attn_sparse(s.L.cache.desc, 64, s.L.slot, s.L.seq_len, s.L.max_seq_len, Q, s.bounds, s.exponents, 3, sel, out)
+    sel, out = sel.cpu().numpy(), out.float().cpu().numpy().astype(np.float64)
+    assert np.all(sel[64:] == -9) and np.all(out[64:] == 7.0) and np.all(np.isfinite(out))
+    for b in (0, 17, 40, 63):
+        first, n = S.packed_range(lengths[b], 4, 64, 1)[2:]
+        for h in range(8):
+            low, up, e = (x[first:first + n] for x in s.oracle_bounds(b, h))
+            qc = [O.query_compensation(s.L.TinvT[h].astype(np.float32), q[b, h * 4 + g][None])[0] for g in range(4)]
+            assert np.array_equal(sel[b, h], S.select(S.page_keys(qc, low, up, e, SCALE), 3, first))
+        _close(out[b], s.oracle_attention(b, q[b], sel[b]))
+    assert s.L.cache.status() == 0
+
+
 def test_a_long_sequence_on_one_head_uses_a_cluster():
     s = Sparse([40000], 2, 1, 2, seed=12)
     s.check(40)
@@ -236,6 +256,16 @@ def test_equal_keys_go_to_the_lower_page():
     sel, out = s.sparse(Q, 6)
     assert np.array_equal(sel, np.broadcast_to(np.arange(6), sel.shape))
     _close(out[0], s.oracle_attention(0, np.zeros_like(q[0]), sel[0]))
+
+
+@pytest.mark.parametrize("n_q,n_kv,bits", [(4, 1, 2), (8, 1, 4)])
+def test_more_listed_pages_than_are_handed_over_in_shared_memory(n_q, n_kv, bits):
+    s = Sparse([45000, 36000], n_q, n_kv, bits, seed=25)
+    q, Q = s.queries()
+    sel, out = s.sparse(Q, 560)
+    assert np.array_equal(sel, s.oracle_select(q, 560))
+    for b in range(2):
+        _close(out[b], s.oracle_attention(b, q[b], sel[b]))
 
 
 def test_lists_of_the_caller():
