@@ -94,6 +94,7 @@ __global__ void __launch_bounds__(256) pages_release_kernel(PoolView v, const in
     for (int i = first + threadIdx.x; i < v.max_pages; i += blockDim.x) drop_page(v, atomicExch(row + i, -1));
 }
 
+// The cluster barriers order all memory accesses, global ones too: what a CTA has written before one is what the others read after it.
 // ---- walks over the pool --------------------------------------------------------------------------------------------------
 // Exclusive prefix sum over the CTA of one number per thread; *total: their sum.
 __device__ __forceinline__ int block_prefix(int x, int* total, int* scratch) {      // scratch: POOL_WARPS ints
@@ -262,7 +263,6 @@ __global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS
             at += total;
         }
     }
-    __threadfence();
     cluster.sync();
 
     // 4. hand them out
@@ -311,7 +311,6 @@ __global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS
         *P.n_copies = written;
         if (!granted) atomicOr(v.dev_status, WUSHKV_DEV_POOL_EMPTY);
     }
-    cluster.sync();                                   // no CTA leaves while another reads its counts
 }
 
 // ---- compact ---------------------------------------------------------------------------------------------------------------
@@ -371,7 +370,6 @@ __global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS
     int holes_here;
     block_prefix(my_holes, &holes_here, scratch);
     if (threadIdx.x == 0) holes_s = holes_here;
-    __threadfence();
     cluster.sync();
     int n_moves = 0;
     for (int r = 0; r < POOL_CTAS; ++r) n_moves += *cluster.map_shared_rank(&holes_s, r);
@@ -388,7 +386,6 @@ __global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS
         P.copy_dst[k] = dst;
     }
     if (rank == 0 && threadIdx.x == 0) { *P.n_copies = n_moves; *P.n_live = live; }
-    __threadfence();
     cluster.sync();
     const long long entries = static_cast<long long>(v.n_slots) * v.max_pages;
 #pragma unroll 4
