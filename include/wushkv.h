@@ -543,7 +543,7 @@ int wushkv_set_profile_events(void* start, void* stop);
  *                       same with a copy of its first token tile (the bounded wait runs out in each case).
  *   "drop_gram"         wushkv_accumulate_gram_device: 1: a CTA's first products are never signalled; 2: one of its first bulk
  *                       copies is announced but never issued (the bounded wait runs out in both cases).
- *   "select_cluster"    1, 2, 4, 8: thread blocks per (sequence, KV head) of the page selection; 0: chosen by the sizes.
+ *   "select_cluster"    1, 2, 4, 8: thread blocks per (sequence, KV head) of sparse attention; -1: one of half the size; 0: chosen by the sizes.
  * Returns WUSHKV_EINVAL for an unknown name.
  */
 int wushkv_set_test_option(const char* name, long long value);

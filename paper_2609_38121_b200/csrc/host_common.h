@@ -61,7 +61,7 @@ struct Knobs {
     int drop_prefill = 0;           // chunk attention: 1 the first tile's score MMAs are never committed, 2 one bulk copy is never issued, 3 one bulk copy of the transform kernel is never issued
     int gram_no_tma = 0;            // 1: the Gram accumulation stages its tiles with 16-byte copies instead of bulk tensor copies
     int drop_gram = 0;              // Gram accumulation: 1 a CTA's first products are never signalled, 2 one of its bulk copies is never issued
-    int select_cluster = 0;         // 1, 2, 4, 8: CTAs per (sequence, KV head) of the page selection; 0: chosen by the sizes
+    int select_cluster = 0;         // 1, 2, 4, 8: CTAs per (sequence, KV head) of sparse attention; -1: one of half the size; 0: chosen by the sizes
     int append_no_tma = 0;          // 1: the chunk append stages its tiles with 16-byte copies instead of bulk tensor copies
 };
 Knobs& knobs();

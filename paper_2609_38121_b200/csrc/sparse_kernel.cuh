@@ -40,11 +40,10 @@ __device__ __forceinline__ void mma_s8(int (&c)[4], unsigned a0, unsigned a1, un
 // CTA 0: key and page id of all pages) and the warps' staging rings.  Where the sizes allow it the rings are apart from the selection's
 // region, so that window tokens can be staged from the start; else the rings begin where the selection's region began.
 constexpr int LISTED = 512;               // listed pages that are handed over in shared memory, with their ids
-constexpr int NT = 256, WARPS = NT / 32;     // threads of a CTA
-template <int MODE>
+template <int MODE, int NT>                  // NT: threads of a CTA
 struct SparseShared {
     static constexpr int GP = MODE == 0 ? 4 : 8, SETS = MODE == 0 ? 1 : 2;
-    static constexpr int BINS = 4 * NT;
+    static constexpr int WARPS = NT / 32, BINS = 4 * NT;
     static constexpr int QF = MODE == 0 ? 64 : 128, QW = MODE == 0 ? 128 : 256;     // uint4 of the attention's integer / bf16 fragments
     union {
         double q[GP][D];                  // the queries, in 64 bits
@@ -235,7 +234,7 @@ __device__ __forceinline__ int bin_of(unsigned key, float per_bin, int n_bins) {
 // is found by a prefix sum and its few keys are compared with each other.
 // The code is kept short: a CTA runs through it once, so that every instruction is fetched for one use (with the keys in registers
 // and its loops unrolled it took 30 KB and was no faster).
-template <class Shared>
+template <int NT, class Shared>
 __device__ __forceinline__ void list_pages(Shared& sh, const uint4& counted, float per_bin, const uint2* keys, int pages, int first, int n_select, int* out) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int c0 = static_cast<int>(counted.x), c1 = static_cast<int>(counted.y), c2 = static_cast<int>(counted.z), here = c0 + c1 + c2 + static_cast<int>(counted.w);
@@ -249,7 +248,7 @@ __device__ __forceinline__ void list_pages(Shared& sh, const uint4& counted, flo
     __syncthreads();
     before -= here;
 #pragma unroll
-    for (int w = 0; w < WARPS; ++w) before += w < warp ? sh.scan[w] : 0;
+    for (int w = 0; w < Shared::WARPS; ++w) before += w < warp ? sh.scan[w] : 0;
     const int rest = n_select - before;                     // the rank, from 1, of the n_select-th key among this thread's bins
     if (rest >= 1 && rest <= here) {
         const int e = (rest > c0) + (rest > c0 + c1) + (rest > c0 + c1 + c2);
@@ -291,7 +290,7 @@ __device__ __forceinline__ void list_pages(Shared& sh, const uint4& counted, flo
             __syncthreads();
             int total = 0;
 #pragma unroll
-            for (int w = 0; w < WARPS; ++w) total += sh.scan[w];
+            for (int w = 0; w < Shared::WARPS; ++w) total += sh.scan[w];
             if (total < n_select) kth = cand;
         }
     }
@@ -306,7 +305,7 @@ __device__ __forceinline__ void list_pages(Shared& sh, const uint4& counted, flo
     __syncthreads();
     int all_below = 0, below_before = 0, equal_before = 0;
 #pragma unroll
-    for (int w = 0; w < WARPS; ++w) {
+    for (int w = 0; w < Shared::WARPS; ++w) {
         const int y = sh.below[w];
         all_below += y;
         if (w < warp) { below_before += y; equal_before += sh.equal[w]; }
@@ -329,7 +328,7 @@ __device__ __forceinline__ void list_pages(Shared& sh, const uint4& counted, flo
     }
 }
 
-// One cluster of CL CTAs per (sequence, KV head).
+// One cluster of CL CTAs per (sequence, KV head); a CTA of NT threads, 512 threads on an SM.
 //   1. q' = T_K^{-T} q: each CTA forms 128 / CL rows of it and hands them to the others through distributed shared memory.
 //   2. Each CTA scores its share of the pages, 16 pages per warp and step: bounds straight from global memory into the A
 //      fragments (their bytes are consecutive in k, so that one 16-byte load per lane and row is two registers of two k-steps).
@@ -340,9 +339,10 @@ __device__ __forceinline__ void list_pages(Shared& sh, const uint4& counted, flo
 //      merged first within the CTAs, then, a CTA per head, over the cluster.
 // Steps 1 to 3 are latency (the bounds of 16 sequences x 8 heads x 510 pages are 17 MB, 2.6 us at the copy rate), step 4 is the
 // work of the dense kernel on fewer pages.
-template <int BITS, int MODE, int CL>
-__global__ void __launch_bounds__(NT, 2) sparse_decode_kernel(SparseParams P) {
-    using Shared = SparseShared<MODE>;
+template <int BITS, int MODE, int CL, int NT>
+__global__ void __launch_bounds__(NT, 512 / NT) sparse_decode_kernel(SparseParams P) {
+    using Shared = SparseShared<MODE, NT>;
+    constexpr int WARPS = Shared::WARPS, HPW = (Shared::GP + WARPS - 1) / WARPS;      // head slots per warp where the warps share them out
     using R = Ring<BITS>;
     constexpr int GP = Shared::GP, SETS = Shared::SETS, NH = WarpState<MODE>::NH;
     extern __shared__ __align__(16) unsigned char sparse_smem[];
@@ -371,8 +371,12 @@ __global__ void __launch_bounds__(NT, 2) sparse_decode_kernel(SparseParams P) {
             for (int r = 0; r < RPT; ++r) tr[r][k] = ld_early(T + r * SPACING * (D / 4) + seg + TPR * (k0 + k));
     };
     load_T(0);
-    uint2 q_bits = make_uint2(0u, 0u);                  // slots without a head are zero
-    if (warp < G) q_bits = ld_in(reinterpret_cast<const uint2*>(P.Q + (static_cast<long long>(b) * c.n_q + h * G + warp) * D + 4 * lane));
+    uint2 q_bits[HPW];                                  // slots without a head are zero
+#pragma unroll
+    for (int k = 0; k < HPW; ++k) {
+        const int head = warp + k * WARPS;
+        q_bits[k] = head < G ? ld_in(reinterpret_cast<const uint2*>(P.Q + (static_cast<long long>(b) * c.n_q + h * G + head) * D + 4 * lane)) : make_uint2(0u, 0u);
+    }
 
     // ---- candidates
     const int S = __ldcg(P.seq_len + b), slot = P.slot[b];
@@ -460,12 +464,15 @@ __global__ void __launch_bounds__(NT, 2) sparse_decode_kernel(SparseParams P) {
     };
     int staged_rows = 0;
 
-    if (warp < GP) {
-        float x[4] = {bf16_bits_to_float(q_bits.x & 0xffff), bf16_bits_to_float(q_bits.x >> 16), bf16_bits_to_float(q_bits.y & 0xffff), bf16_bits_to_float(q_bits.y >> 16)};
-        if (warp < G && P.pro.rope)
-            norm_rope_warp(x, lane, P.pro, h * G + warp, prologue_position(P.pro, max(S - 1, 0), c.dev_status, lane == 0 && rank == 0));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sh.q[warp][4 * lane + e] = static_cast<double>(x[e]);
+    for (int k = 0; k < HPW; ++k) {
+        const int head = warp + k * WARPS;
+        if (head >= GP) break;
+        float x[4] = {bf16_bits_to_float(q_bits[k].x & 0xffff), bf16_bits_to_float(q_bits[k].x >> 16), bf16_bits_to_float(q_bits[k].y & 0xffff), bf16_bits_to_float(q_bits[k].y >> 16)};
+        if (head < G && P.pro.rope)
+            norm_rope_warp(x, lane, P.pro, h * G + head, prologue_position(P.pro, max(S - 1, 0), c.dev_status, lane == 0 && rank == 0));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sh.q[head][4 * lane + e] = static_cast<double>(x[e]);
     }
     __syncthreads();
     BoundsTile tile;
@@ -506,11 +513,12 @@ __global__ void __launch_bounds__(NT, 2) sparse_decode_kernel(SparseParams P) {
 
     // ---- the query as two signed bytes per channel: q' ~ (max|q'| / 32512) (256 hi + lo), in B fragments.  A warp per column pair (or
     // column) of a head; the queries of head slots without a head are zero, and so are their columns.
-    if (warp < GP) {
+#pragma unroll 1
+    for (int head = warp; head < GP; head += WARPS) {
         double x[4], most = 0.0;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {                            // from the CTA whose rows they are
-            const double2* from = reinterpret_cast<const double2*>(&sh.qc[warp][4 * lane + 2 * e]);
+            const double2* from = reinterpret_cast<const double2*>(&sh.qc[head][4 * lane + 2 * e]);
             const double2 v = *(CL > 1 ? cluster.map_shared_rank(from, 4 * lane / ROWS) : from);
             x[2 * e] = v.x; x[2 * e + 1] = v.y;
             most = fmax(most, fmax(fabs(v.x), fabs(v.y)));
@@ -538,11 +546,11 @@ __global__ void __launch_bounds__(NT, 2) sparse_decode_kernel(SparseParams P) {
         for (int side = 0; side < 2; ++side)
 #pragma unroll
             for (int digit = 0; digit < 2; ++digit) {
-                const int set = MODE == 0 ? 0 : digit, column = MODE == 0 ? 2 * warp + digit : warp;
+                const int set = MODE == 0 ? 0 : digit, column = MODE == 0 ? 2 * head + digit : head;
                 const int group = 2 * side + lane / 16, tl = (lane % 16) / 4;
                 frag[((set * 4 + group) * 32 + 4 * column + tl) * 4 + lane % 4] = word[side][digit];
             }
-        if (lane == 0) sh.unit[warp] = usable ? static_cast<float>(__dmul_rn(most / QM, static_cast<double>(c.sm_scale))) : 0.f;
+        if (lane == 0) sh.unit[head] = usable ? static_cast<float>(__dmul_rn(most / QM, static_cast<double>(c.sm_scale))) : 0.f;
         if (attend) {
             // what decode_prep_kernel makes of q' (there from fp32 sums): digits in integer fragments, q' in the scale of the scores'
             // base-2 exponent as bf16 value and remainder, two scalars per head
@@ -554,7 +562,7 @@ __global__ void __launch_bounds__(NT, 2) sparse_decode_kernel(SparseParams P) {
                 const int ch = 4 * lane + 2 * k, s = ch >> 5, hh = (ch >> 4) & 1, u = (ch >> 3) & 1, tq = (ch >> 1) & 3;
 #pragma unroll
                 for (int digit = 0; digit < 2; ++digit) {
-                    const int set = MODE == 0 ? 0 : digit, column = MODE == 0 ? 2 * warp + digit : warp;
+                    const int set = MODE == 0 ? 0 : digit, column = MODE == 0 ? 2 * head + digit : head;
                     ifrag[set * 512 + (((s >> 1) * 32 + 4 * column + tq) * 16 + ((s & 1) * 2 + hh) * 4 + 2 * u) / 2] = static_cast<unsigned short>(digits[digit] >> (16 * k));
                 }
                 const int s16 = ch >> 4, r = (ch >> 3) & 1;
@@ -566,14 +574,14 @@ __global__ void __launch_bounds__(NT, 2) sparse_decode_kernel(SparseParams P) {
                 }
 #pragma unroll
                 for (int part = 0; part < 2; ++part) {
-                    const int set = MODE == 0 ? 0 : part, column = MODE == 0 ? 2 * warp + part : warp;
+                    const int set = MODE == 0 ? 0 : part, column = MODE == 0 ? 2 * head + part : head;
                     const float a = part == 0 ? y[0] : rest[0], d = part == 0 ? y[1] : rest[1];
                     wfrag[set * 512 + ((s16 >> 1) * 32 + 4 * column + tq) * 4 + (s16 & 1) * 2 + r] = float_to_bf16_bits(a) | (static_cast<unsigned>(float_to_bf16_bits(d)) << 16);
                 }
             }
             sum = __reduce_add_sync(FULL, sum);
             constexpr float FS = BITS != 4 ? 4.f : 16.f;        // the integer score carries this factor (page_scores)
-            if (lane == 0) sh.scal[warp] = make_float2(k2 * lam * (1.f / FS), FS * static_cast<float>(sum));
+            if (lane == 0) sh.scal[head] = make_float2(k2 * lam * (1.f / FS), FS * static_cast<float>(sum));
         }
     }
     __syncthreads();
@@ -667,7 +675,7 @@ __global__ void __launch_bounds__(NT, 2) sparse_decode_kernel(SparseParams P) {
                 const uint4 x = *(CL > 1 ? cluster.map_shared_rank(&sh.bins[tid], r) : &sh.bins[tid]);
                 counted.x += x.x; counted.y += x.y; counted.z += x.z; counted.w += x.w;
             }
-            list_pages(sh, counted, per_bin, keys, pages, first, P.n_select, list);
+            list_pages<NT>(sh, counted, per_bin, keys, pages, first, P.n_select, list);
         }
         if (!attend) {
             if (CL > 1) cluster.sync();                         // no CTA leaves while its bins are read
@@ -798,16 +806,17 @@ __global__ void __launch_bounds__(NT, 2) sparse_decode_kernel(SparseParams P) {
         copies_wait<0>();
     }
 
-    // ---- merge: the CTA's eight states, then the cluster's
+    // ---- merge: the states of the CTA's warps, then the cluster's
     __syncwarp();
     store_state<BITS, MODE, false>(st, reinterpret_cast<float*>(ring), lane, G);
     __syncthreads();                                             // sh.attn has been read, too
-    if (warp < G) {
+#pragma unroll 1
+    for (int head = warp; head < G; head += WARPS) {
         MergedState ms;
         ms.reset();
-        ms.add<false>(WARPS, lane, [&](int k) { return reinterpret_cast<const float*>(rings + k * R::BYTES) + warp * PART_STRIDE; });
-        if (CL > 1) ms.store(sh.merged[warp], lane);
-        else ms.finish(P.O + (static_cast<long long>(b) * c.n_q + h * G + warp) * D, lane);
+        ms.add<false>(WARPS, lane, [&](int k) { return reinterpret_cast<const float*>(rings + k * R::BYTES) + head * PART_STRIDE; });
+        if (CL > 1) ms.store(sh.merged[head], lane);
+        else ms.finish(P.O + (static_cast<long long>(b) * c.n_q + h * G + head) * D, lane);
     }
     if (CL > 1) {
         cluster.sync();
@@ -823,26 +832,26 @@ __global__ void __launch_bounds__(NT, 2) sparse_decode_kernel(SparseParams P) {
     }
 }
 
-constexpr int SPARSE_SMEM_MAX = 226 * 1024, SPARSE_SMEM_HALF = 113 * 1024;      // of a CTA; of one of two on an SM
+constexpr int SPARSE_SMEM_MAX = 226 * 1024;
 __host__ __device__ constexpr size_t scored_bytes(size_t group, size_t per, size_t pages) { return (4 * (1 + group) * per + 8 * pages + 15) / 16 * 16; }
 
 // Shared memory of a CTA and where in it the rings begin.
-template <int BITS, int MODE>
+template <int BITS, int MODE, int NT>
 static size_t sparse_smem(const SparseParams& P, int cl, int& ring_offset) {
-    constexpr size_t shared = sizeof(SparseShared<MODE>);
+    constexpr size_t shared = sizeof(SparseShared<MODE, NT>);
     static_assert(shared + scored_bytes(MODE == 0 ? 4 : 8, MAX_SELECT_PAGES / 8, MAX_SELECT_PAGES) <= SPARSE_SMEM_MAX, "clusters of 8 hold every allowed number of pages");
     const size_t scored = P.bounds ? scored_bytes(P.c.G, pages_per_cta(P.max_candidates, cl), P.max_candidates) : 0;
-    const size_t ring = P.O ? WARPS * Ring<BITS>::BYTES : 0, apart = shared + scored + ring;
-    // apart from the scores unless that costs the second CTA of an SM one that would come
+    const size_t ring = P.O ? NT / 32 * Ring<BITS>::BYTES : 0, apart = shared + scored + ring;
+    // apart from the scores unless that costs an SM one of the CTAs that its registers hold and that would come
     const bool alone = static_cast<long long>(P.batch) * P.c.n_kv * cl <= sm_count();
     ring_offset = 0;
-    if (scored > 0 && ring > 0 && apart <= (alone ? SPARSE_SMEM_MAX : SPARSE_SMEM_HALF)) { ring_offset = static_cast<int>(scored); return apart; }
+    if (scored > 0 && ring > 0 && apart <= (alone ? SPARSE_SMEM_MAX : SPARSE_SMEM_MAX / (512 / NT))) { ring_offset = static_cast<int>(scored); return apart; }
     return shared + std::max(scored, ring);
 }
 
-template <int BITS, int MODE, int CL>
+template <int BITS, int MODE, int CL, int NT>
 static int launch_sparse_cl(SparseParams P, cudaStream_t st) {
-    const auto kernel = sparse_decode_kernel<BITS, MODE, CL>;
+    const auto kernel = sparse_decode_kernel<BITS, MODE, CL, NT>;
     if (!opt_in_dynamic_smem(reinterpret_cast<const void*>(kernel), SPARSE_SMEM_MAX)) return WUSHKV_ECUDA;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -852,7 +861,7 @@ static int launch_sparse_cl(SparseParams P, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(CL, P.c.n_kv, P.batch);
     cfg.blockDim = dim3(NT);
-    cfg.dynamicSmemBytes = sparse_smem<BITS, MODE>(P, CL, P.ring_offset);
+    cfg.dynamicSmemBytes = sparse_smem<BITS, MODE, NT>(P, CL, P.ring_offset);
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = CL > 1 ? 2 : 1;
@@ -868,14 +877,21 @@ static int launch_sparse_mode(const SparseParams& P, cudaStream_t st) {
     const long long pairs = static_cast<long long>(P.batch) * P.c.n_kv;
     const long long work = std::max<long long>(P.bounds ? P.max_candidates / 16 : 0, P.O ? P.n_select / 2 : 0);
     int offset, cl = knobs().select_cluster;
+    // More pairs than CTAs of 8 warps are resident: CTAs of 4 warps, so that pairs in different steps overlap (64 ragged sequences x 8
+    // heads, 4 bits: 50.3 -> 43.8 us; 352 to 1024 pairs of 4 query heads 2 to 8 % faster, one case 1 % slower; 128 to 288 pairs 8 to 30 %
+    // slower).  With more than 4 query heads the fixed part of a pair is too long for 4 warps (512 pairs: 51.0 against 60.3 us).
+    if constexpr (MODE == 0) {
+        const bool small = cl == 0 ? pairs > 2 * sm_count() : cl == -1;
+        if (small && sparse_smem<BITS, MODE, 128>(P, 1, offset) <= SPARSE_SMEM_MAX / 2) return launch_sparse_cl<BITS, MODE, 1, 128>(P, st);
+    }
     if (cl != 2 && cl != 4 && cl != 8) cl = 1;
-    while (knobs().select_cluster == 0 && cl < 8 && 2 * pairs * cl <= sm_count() && work > WARPS * cl) cl *= 2;
-    while (cl < 8 && sparse_smem<BITS, MODE>(P, cl, offset) > SPARSE_SMEM_MAX) cl *= 2;      // the scores and keys have to fit
+    while (knobs().select_cluster == 0 && cl < 8 && 2 * pairs * cl <= sm_count() && work > 8 * cl) cl *= 2;
+    while (cl < 8 && sparse_smem<BITS, MODE, 256>(P, cl, offset) > SPARSE_SMEM_MAX) cl *= 2;      // the scores and keys have to fit
     switch (cl) {
-        case 1: return launch_sparse_cl<BITS, MODE, 1>(P, st);
-        case 2: return launch_sparse_cl<BITS, MODE, 2>(P, st);
-        case 4: return launch_sparse_cl<BITS, MODE, 4>(P, st);
-        default: return launch_sparse_cl<BITS, MODE, 8>(P, st);
+        case 1: return launch_sparse_cl<BITS, MODE, 1, 256>(P, st);
+        case 2: return launch_sparse_cl<BITS, MODE, 2, 256>(P, st);
+        case 4: return launch_sparse_cl<BITS, MODE, 4, 256>(P, st);
+        default: return launch_sparse_cl<BITS, MODE, 8, 256>(P, st);
     }
 }
 

@@ -227,7 +227,7 @@ def test_every_cluster_size_selects_the_same(n_q, n_kv):
     ref = s.oracle_select(q, 624)
     for n_select in (1, 40, 150, 300, 624):
         want = ref if n_select == 624 else s.oracle_select(q, n_select)
-        for cluster in (1, 2, 4, 8, 0):
+        for cluster in (-1, 1, 2, 4, 8, 0):
             s.B.set_test_option("select_cluster", cluster)
             try:
                 sel = s.torch.full((3, n_kv, n_select), -9, dtype=s.torch.int32, device="cuda")
