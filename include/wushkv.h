@@ -11,6 +11,8 @@
  *   (3) decode attention over that packed cache for one new query per sequence
  *       (Algorithm 2 lines 3 and 5; Eq. 2; Eq. 3), reading the first S_sink and the most
  *       recent positions from a bf16 copy (Section 4.4).
+ *   (4) sparse decode attention: the windows and those packed pages whose bounds promise the largest scores,
+ *   (5) management of the pages: reserving, sharing, releasing and compacting them, with the copies that follow.
  *
  * General rules
  *   - Every function returns an int status (WUSHKV_OK = 0).  No exceptions.  Global state is
@@ -19,7 +21,7 @@
  *   - "host" / "device" beside a pointer says where the memory must live.  All memory is
  *     owned by the caller before, during and after every call; the library allocates nothing
  *     and keeps no pointer between calls.
- *   - wushkv_append / wushkv_decode_attn / wushkv_unpack_debug only ENQUEUE work on the CUDA
+ *   - Calls that take a stream (wushkv_append, wushkv_decode_attn, ...) only ENQUEUE work on the CUDA
  *     stream passed in (a cudaStream_t cast to void*, NULL = default stream) and do not
  *     synchronise.  Arguments are validated on the host before anything is launched; a bad
  *     argument returns WUSHKV_EINVAL and launches nothing.
@@ -407,7 +409,7 @@ int wushkv_decode_step_host(const wushkv_cache* cache, int32_t batch, const int3
  * wushkv_decode_attn_sparse is both in one launch.  selected may be NULL there: the list is then kept in workspace (device,
  * 256-byte aligned, >= wushkv_sparse_workspace_bytes() bytes, scratch), which is not used otherwise and may then be NULL.
  * prologue: NULL, or the Norm / RoPE of projected queries (as in wushkv_decode_attn_projected).
- * The other arguments are those of wushkv_decode_attn.  A sequence may be named by several rows of a call with different lengths
+ * The other arguments, and the range of the stored value steps, are those of wushkv_decode_attn.  A sequence may be named by several rows of a call with different lengths
  * (tokens to verify), as long as the ring still holds the recent window of the shortest.
  */
 int wushkv_update_page_bounds(const wushkv_cache* cache, int32_t batch, const int32_t* slot, const int32_t* seq_len,
