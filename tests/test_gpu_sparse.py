@@ -402,6 +402,47 @@ def test_pages_far_behind_in_a_large_pool():
     assert np.array_equal(sel, sel0) and np.array_equal(out, out0)
 
 
+@pytest.mark.parametrize("n_q,n_kv,bits", [(8, 1, 2), (2, 1, 4), (6, 2, 3)])
+def test_a_million_positions(n_q, n_kv, bits):
+    """The longest sequences there may be: 16383 candidate pages, drawn bounds, packed tokens whose keys and values are zero."""
+    import torch
+    from paper_2609_38121_b200 import binding as B
+    rng, longest, n_select = np.random.default_rng(bits), 1 << 20, 700
+    T = np.stack([np.linalg.qr(rng.standard_normal((128, 128)))[0] for _ in range(n_kv)]).astype(np.float32)
+    c = B.PagedCache(n_q, n_kv, bits, 2, longest, 4, 64, 1, 0.96, 0.92, T, T, page_order=rng.permutation(2 * 16384), page_bounds=True)
+    gen = torch.Generator(device="cuda").manual_seed(bits)
+    up = torch.randint(20, 127, c.bounds.shape[:2] + (128,), generator=gen, device="cuda", dtype=torch.int32)
+    low = -torch.randint(20, 127, up.shape, generator=gen, device="cuda", dtype=torch.int32)
+    c.bounds.copy_(torch.stack([low, up], 2))
+    c.exponents.copy_(torch.randint(-6, -4, c.exponents.shape, generator=gen, device="cuda"))
+    for t in (c.ring_kv, c.sink_kv):
+        t.copy_(torch.randn(t.shape, generator=gen, device="cuda"))
+    lens = [longest, 999_937]
+    q = W.bf16_round_f32(rng.standard_normal((2, n_q, 128)).astype(np.float32) * 2)
+    Q = torch.from_numpy(W.f32_to_bf16_bits(q).view(np.int16)).cuda()
+    slot, seq_len = torch.arange(2, dtype=torch.int32, device="cuda"), torch.tensor(lens, dtype=torch.int32, device="cuda")
+    sel, out = torch.zeros((2, n_kv, n_select), dtype=torch.int32, device="cuda"), torch.zeros((2, n_q, 128), dtype=torch.bfloat16, device="cuda")
+    B.decode_attn_sparse(c.desc, 2, slot, seq_len, longest, Q, c.bounds, c.exponents, n_select, sel, out)
+    assert c.status() == 0
+    sel, out, table, G = sel.cpu().numpy(), out.float().cpu().numpy().astype(np.float64), c.page_table.cpu().numpy(), n_q // n_kv
+    bounds, e = c.bounds.cpu().numpy().astype(int), c.exponents.cpu().numpy().astype(int)
+    ring, sink = c.ring_kv.float().cpu().numpy().astype(np.float64), c.sink_kv.float().cpu().numpy().astype(np.float64)
+    for b in range(2):
+        lo, hi, first, n = S.packed_range(lens[b], 4, 64, 1)
+        for h in range(n_kv):
+            row = table[b, first:first + n]
+            qc = [O.query_compensation(T[h], q[b, h * G + g][None])[0] for g in range(G)]
+            assert np.array_equal(sel[b, h], S.select(S.page_keys(qc, bounds[row, h, 0], bounds[row, h, 1], e[row, h], SCALE), n_select, first))
+            packed = sum(min(hi, 64 * p + 64) - max(lo, 64 * p) for p in sel[b, h])
+            rows = [p % c.ring_cap for p in range(hi, lens[b])]
+            K, V = (np.concatenate([sink[b, h, i], ring[b, h, i][rows]]) for i in range(2))
+            ref = []
+            for x in qc:
+                p = np.exp(SCALE * (K @ x))
+                ref.append(p @ V / (p.sum() + packed))
+            _close(out[b, h * G:(h + 1) * G], np.stack(ref))
+
+
 def test_captured_steps_and_other_streams():
     """A decode step of append, bounds and sparse attention, captured once and replayed over growing sequences, on a stream of its
     own: the results of the separate calls."""
