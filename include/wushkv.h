@@ -435,6 +435,7 @@ int wushkv_decode_attn_sparse(const wushkv_cache* cache, int32_t batch, const in
  *     the pool (BAD_PAGE_ID).
  *   refs (device, in/out): int32 [n_pages], number of table entries that name the page; 0: the page is free.
  *   dev_status (device): error bits, as in wushkv_cache.
+ *   n_pages <= 2^30, max_pages <= 2^20; batch <= 2^30 in the calls below (EINVAL otherwise).
  * The caller starts with a table of -1 and counts of 0 (or with counts that match its table).
  *
  * wushkv_pages_reserve: before wushkv_append of the tokens (seq_len, cu_new as the append will get them), gives every sequence

@@ -174,7 +174,8 @@ __global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS
     const int rank = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     __shared__ int scratch[POOL_WARPS];
     __shared__ int tile[POOL_THREADS];
-    __shared__ int free_s, total_s, copies_s;            // free pages of this CTA's part; CTA 0: pages and copies asked for
+    __shared__ int free_s, copies_s;                     // free pages of this CTA's part; CTA 0: copies asked for
+    __shared__ long long total_s;                        // CTA 0: pages asked for
 
     // 1. what every sequence needs: a warp per sequence, a lane per page index
     for (int b = rank * POOL_WARPS + warp; b < P.batch; b += POOL_CTAS * POOL_WARPS) {
@@ -207,7 +208,8 @@ __global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS
     // 2. CTA 0: which shared pages are copied, and the first rank of every sequence.  The sequences are taken in order: one that
     // finds its page still shared copies it and leaves it, so of k holders of a page that are all here the last one keeps it.
     if (rank == 0) {
-        int pages = 0, copies = 0;
+        long long pages = 0;
+        int copies = 0;
         for (int base = 0; base < P.batch; base += POOL_THREADS) {
             const int b = base + threadIdx.x;
             int need = 0, shared = -1;
@@ -231,14 +233,15 @@ __global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS
             int total_p, total_c;
             const int at = block_prefix(need + (copy ? 1 : 0), &total_p, scratch);
             const int at_copy = block_prefix(copy ? 1 : 0, &total_c, scratch);
-            if (b < P.batch) { P.need[b] = pages + at; P.shared[b] = copy ? 1 + copies + at_copy : 0; }
+            if (b < P.batch) { P.need[b] = static_cast<int>(pages) + at; P.shared[b] = copy ? 1 + copies + at_copy : 0; }
             pages += total_p;
             copies += total_c;
         }
         if (threadIdx.x == 0) { total_s = pages; copies_s = copies; }
     }
     cluster.sync();
-    const int wanted = *cluster.map_shared_rank(&total_s, 0), copies = *cluster.map_shared_rank(&copies_s, 0);
+    const long long wanted = *cluster.map_shared_rank(&total_s, 0);
+    const int copies = *cluster.map_shared_rank(&copies_s, 0);
     int free_before = 0, free_all = 0;
     for (int r = 0; r < POOL_CTAS; ++r) {
         const int f = *cluster.map_shared_rank(&free_s, r);
@@ -494,8 +497,15 @@ __global__ void __launch_bounds__(256) copy_windows_kernel(CopyWindowsParams P) 
     for (int e = 0; e < WINDOW_VECS; ++e) if (to[e]) *to[e] = x[e];
 }
 
+// The kernels walk pages and requests with 32-bit indexes that run past the end by up to a step, and add up the pages that a tile
+// of POOL_THREADS requests asks for in 32 bits.
+constexpr long long MAX_POOL_PAGES = 1 << 30;
+constexpr int MAX_POOL_BATCH = 1 << 30, MAX_TABLE_PAGES = 1 << 20;
+static_assert(POOL_THREADS * (MAX_TABLE_PAGES + 1ll) < 0x7fffffffll, "a tile's pages are counted in 32 bits");
+
 static int make_pool(const wushkv_page_pool* p, PoolView& v) {
-    if (!p || p->n_slots <= 0 || p->max_pages <= 0 || p->n_pages <= 0 || p->n_pages > 0x7ffffff0ll) return WUSHKV_EINVAL;
+    if (!p || p->n_slots <= 0 || p->max_pages <= 0 || p->n_pages <= 0) return WUSHKV_EINVAL;
+    if (p->n_pages > MAX_POOL_PAGES || p->max_pages > MAX_TABLE_PAGES) return WUSHKV_EINVAL;
     if (!p->page_table || !p->refs || !p->dev_status) return WUSHKV_EINVAL;
     if (!aligned(p->page_table, 4) || !aligned(p->refs, 4) || !aligned(p->dev_status, 4)) return WUSHKV_EINVAL;
     v.n_slots = p->n_slots; v.max_pages = p->max_pages; v.n_pages = static_cast<int>(p->n_pages);
@@ -517,7 +527,7 @@ using namespace wushkv;
 
 extern "C" size_t wushkv_pages_workspace_bytes(const wushkv_page_pool* pool, int32_t batch) {
     PoolView v;
-    if (make_pool(pool, v) != WUSHKV_OK || batch <= 0) return 0;
+    if (make_pool(pool, v) != WUSHKV_OK || batch <= 0 || batch > MAX_POOL_BATCH) return 0;
     return pool_workspace_ints(v, batch) * sizeof(int);
 }
 
@@ -526,7 +536,7 @@ extern "C" int wushkv_pages_reserve(const wushkv_page_pool* pool, int32_t batch,
     ReserveParams P;
     const int rc = make_pool(pool, P.v);
     if (rc != WUSHKV_OK) return rc;
-    if (batch <= 0 || !slot || !seq_len || !cu_new || !copy_src || !copy_dst || !n_copies || !workspace || !aligned(workspace, 4)) return WUSHKV_EINVAL;
+    if (batch <= 0 || batch > MAX_POOL_BATCH || !slot || !seq_len || !cu_new || !copy_src || !copy_dst || !n_copies || !workspace || !aligned(workspace, 4)) return WUSHKV_EINVAL;
     if (workspace_bytes < pool_workspace_ints(P.v, batch) * sizeof(int)) return WUSHKV_ECAPACITY;
     P.batch = batch; P.slot = slot; P.seq_len = seq_len; P.cu_new = cu_new;
     P.copy_src = copy_src; P.copy_dst = copy_dst; P.n_copies = n_copies;

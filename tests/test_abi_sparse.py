@@ -52,7 +52,7 @@ REFUSED = [
     (B.lib.wushkv_decode_attn_sparse, SPARSE, dict(cache=[None], batch=[0, 65536], bounds=[None, P + 4], exponents=[None], n_select=[0], O=[None, P + 8])),
     (B.lib.wushkv_decode_attn_sparse, {**SPARSE, "selected": None}, dict(cache=[None, _cache(bits=1)], batch=[0], n_select=[0], max_seq_len=[0], ws=[None, P + 128])),
     (B.lib.wushkv_pages_reserve, RESERVE, dict(pool=[None, _pool(n_pages=0), _pool(n_slots=0), _pool(max_pages=-1), _pool(refs=None), _pool(page_table=P + 2),
-                                                     _pool(dev_status=None), _pool(n_pages=1 << 31)], batch=[0, -2], slot=[None], seq_len=[None], cu_new=[None],
+                                                     _pool(dev_status=None), _pool(n_pages=1 << 31), _pool(n_pages=(1 << 30) + 1), _pool(max_pages=(1 << 20) + 1)], batch=[0, -2, (1 << 30) + 1], slot=[None], seq_len=[None], cu_new=[None],
                                                copy_src=[None], copy_dst=[None], n_copies=[None], ws=[None, P + 1])),
     (B.lib.wushkv_pages_fork, FORK, dict(pool=[None], n=[-1], src=[None], dst=[None], src_len=[None])),
     (B.lib.wushkv_pages_release, RELEASE, dict(pool=[None], n=[-1], slot=[None])),
