@@ -390,7 +390,7 @@ int wushkv_decode_step_host(const wushkv_cache* cache, int32_t batch, const int3
  *
  * Selection.  wushkv_select_pages lists, per sequence and KV head, min(n_select, packed pages) page indexes (of the page table's
  * row) in ascending order, -1 in the places behind:
- *   selected (device, out): int32 [batch][n_kv][n_select].
+ *   selected (device, out): int32 [batch][n_kv][n_select]; n_select <= 2^30.
  * q' = T_K^{-T} q (double precision) is rounded to qi = round(q' * 32512 / max|q'|).  The score of a page for a query head is
  *   s = 2^e * sum_c (max(qi_c, 0) upper_c + min(qi_c, 0) lower_c) * (max|q'| / 32512 * sm_scale),
  * an upper bound of the logits of all its tokens (for the rounded query); the sum is an exact integer, s is rounded to fp32

@@ -179,13 +179,15 @@ static long long candidate_bound(const CacheView& c, int max_seq_len) {
     return nq > 0 ? (c.s_sink + nq - 1) / PAGE_TOKENS - c.s_sink / PAGE_TOKENS + 1 : 0;
 }
 
+constexpr int MAX_LIST = 1 << 30;      // the kernel's walk over a list ends up to a step behind it, in 32 bits
+
 // Checks and launches all three calls: bounds == nullptr: the list is an input; O == nullptr: the list is all that is asked for.
 static int sparse_impl(const wushkv_cache* cache, int32_t batch, const int32_t* slot, const int32_t* seq_len, int32_t max_seq_len, const uint16_t* Q,
                        const wushkv_prologue* prologue, const int8_t* bounds, const int8_t* exponents, int32_t n_select, int32_t* selected, uint16_t* O, void* stream) {
     SparseParams P;
     const int rc = make_view(cache, P.c);
     if (rc != WUSHKV_OK) return rc;
-    if (batch <= 0 || batch > 65535 || P.c.n_kv > 65535 || max_seq_len <= 0 || n_select <= 0) return WUSHKV_EINVAL;
+    if (batch <= 0 || batch > 65535 || P.c.n_kv > 65535 || max_seq_len <= 0 || n_select <= 0 || n_select > MAX_LIST) return WUSHKV_EINVAL;
     if (!slot || !seq_len || !Q || !selected || !aligned(Q, 16) || !aligned(bounds, 16) || !aligned(O, 16)) return WUSHKV_EINVAL;
     P.pro = Prologue{nullptr, 0, 0, nullptr, 0.f};
     if (prologue && !make_prologue(prologue, prologue->q_norm_weight, P.pro)) return WUSHKV_EINVAL;
@@ -236,7 +238,7 @@ extern "C" int wushkv_decode_attn_selected(const wushkv_cache* cache, int32_t ba
 
 extern "C" size_t wushkv_sparse_workspace_bytes(const wushkv_cache* cache, int32_t batch, int32_t max_seq_len, int32_t n_select) {
     CacheView v;
-    if (make_view(cache, v) != WUSHKV_OK || batch <= 0 || max_seq_len <= 0 || n_select <= 0) return 0;
+    if (make_view(cache, v) != WUSHKV_OK || batch <= 0 || max_seq_len <= 0 || n_select <= 0 || n_select > MAX_LIST) return 0;
     return (static_cast<size_t>(batch) * v.n_kv * n_select * sizeof(int32_t) + 255) / 256 * 256;
 }
 

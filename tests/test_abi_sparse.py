@@ -46,10 +46,10 @@ REFUSED = [
     (B.lib.wushkv_update_page_bounds, BOUNDS, dict(cache=[None, _cache(bits=5), _cache(d=64), _cache(n_q=9), _cache(pages=None)], batch=[0, -1, 65536], slot=[None],
                                                    seq_len=[None], cu_new=[None], max_new=[-1], bounds=[None, P + 8], exponents=[None])),
     (B.lib.wushkv_select_pages, SELECT, dict(cache=[None, _cache(n_kv=0)], batch=[0, 65536], slot=[None], seq_len=[None], max_seq_len=[0, -5], Q=[None, P + 2],
-                                             bounds=[None, P + 1], exponents=[None], n_select=[0, -1], selected=[None], prologue=[C.byref(B.wushkv_prologue())])),
+                                             bounds=[None, P + 1], exponents=[None], n_select=[0, -1, (1 << 30) + 1], selected=[None], prologue=[C.byref(B.wushkv_prologue())])),
     (B.lib.wushkv_decode_attn_selected, ATTEND, dict(cache=[None], batch=[0, 65536], slot=[None], seq_len=[None], max_seq_len=[0], Q=[None, P + 8], selected=[None],
-                                                     n_select=[0], O=[None, P + 2], prologue=[C.byref(B.wushkv_prologue())])),
-    (B.lib.wushkv_decode_attn_sparse, SPARSE, dict(cache=[None], batch=[0, 65536], bounds=[None, P + 4], exponents=[None], n_select=[0], O=[None, P + 8])),
+                                                     n_select=[0, (1 << 30) + 1], O=[None, P + 2], prologue=[C.byref(B.wushkv_prologue())])),
+    (B.lib.wushkv_decode_attn_sparse, SPARSE, dict(cache=[None], batch=[0, 65536], bounds=[None, P + 4], exponents=[None], n_select=[0, (1 << 30) + 1], O=[None, P + 8])),
     (B.lib.wushkv_decode_attn_sparse, {**SPARSE, "selected": None}, dict(cache=[None, _cache(bits=1)], batch=[0], n_select=[0], max_seq_len=[0], ws=[None, P + 128])),
     (B.lib.wushkv_pages_reserve, RESERVE, dict(pool=[None, _pool(n_pages=0), _pool(n_slots=0), _pool(max_pages=-1), _pool(refs=None), _pool(page_table=P + 2),
                                                      _pool(dev_status=None), _pool(n_pages=1 << 31), _pool(n_pages=(1 << 30) + 1), _pool(max_pages=(1 << 20) + 1)], batch=[0, -2, (1 << 30) + 1], slot=[None], seq_len=[None], cu_new=[None],
