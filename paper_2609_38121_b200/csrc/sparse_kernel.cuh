@@ -357,9 +357,12 @@ __global__ void __launch_bounds__(NT, 512 / NT) sparse_decode_kernel(SparseParam
     pdl_launch_dependents();
     if (tid == 0) sh.n_list = 0;
     // ---- q': this thread's rows of T_K^{-T} and its share of the queries are requested ahead of everything else
-    constexpr int ROWS = D / CL, RPT = 2;                                                     // rows per thread: a query element read from shared memory serves both
+    // Rows per thread: a query element read from shared memory serves all of them.  Four with CTAs of four warps, whose SMs are busy with
+    // other pairs meanwhile (64 ragged sequences x 8 heads: 43.8 -> 42.2 us); two where the chain of one CTA counts (with four rows 1 x 2k
+    // tokens take the same 9.9 us, 16 x 32k 26.9 instead of 26.75 us, the selection alone 9.6 instead of 9.3 us).
+    constexpr int ROWS = D / CL, RPT = NT == 128 ? 4 : 2;
     constexpr int SPACING = ROWS / RPT, TPR = NT / SPACING, QUADS = D / 4 / TPR;              // rows apart, threads per row, float4 per thread and row
-    constexpr int PART = QUADS > 4 ? 4 : QUADS;                                              // of them in flight together
+    constexpr int PART = QUADS * RPT > 8 ? 8 / RPT : QUADS;                                  // of them in flight together
     static_assert(TPR <= 32 && QUADS >= 1 && QUADS % PART == 0, "a row is summed within a warp");
     const int t_row = rank * ROWS + tid / TPR, seg = tid % TPR;
     const uint4* T = reinterpret_cast<const uint4*>(c.T_K_invT + (static_cast<long long>(h) * D + t_row) * D);
@@ -878,7 +881,7 @@ static int launch_sparse_mode(const SparseParams& P, cudaStream_t st) {
     const long long work = std::max<long long>(P.bounds ? P.max_candidates / 16 : 0, P.O ? P.n_select / 2 : 0);
     int offset, cl = knobs().select_cluster;
     // More pairs than CTAs of 8 warps are resident: CTAs of 4 warps, so that pairs in different steps overlap (64 ragged sequences x 8
-    // heads, 4 bits: 50.3 -> 43.8 us; 352 to 1024 pairs of 4 query heads 2 to 8 % faster, one case 1 % slower; 128 to 288 pairs 8 to 30 %
+    // heads, 4 bits: 50.3 -> 42.2 us; 352 to 1024 pairs of 4 query heads 2 to 8 % faster, one case 1 % slower; 128 to 288 pairs 8 to 30 %
     // slower).  With more than 4 query heads the fixed part of a pair is too long for 4 warps (512 pairs: 51.0 against 60.3 us).
     if constexpr (MODE == 0) {
         const bool small = cl == 0 ? pairs > 2 * sm_count() : cl == -1;
