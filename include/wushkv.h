@@ -63,8 +63,8 @@ extern "C" {
 #define WUSHKV_QUANTIZER_QUEST  1
 
 /* ---- bits OR-ed into *dev_status by kernels ---------------------------------------------- */
-#define WUSHKV_DEV_PAGE_TABLE_FULL 1  /* a position needs page index >= max_pages: token skipped */
-#define WUSHKV_DEV_BAD_PAGE_ID     2  /* page table entry outside [0, n_pages): access skipped   */
+#define WUSHKV_DEV_PAGE_TABLE_FULL 1  /* a position needs page index >= max_pages: access skipped, an append's sequence refused */
+#define WUSHKV_DEV_BAD_PAGE_ID     2  /* page table entry outside [0, n_pages): access skipped, an append's sequence refused */
 #define WUSHKV_DEV_BAD_SLOT        4  /* slot[b] outside [0, n_slots): sequence skipped          */
 #define WUSHKV_DEV_COPY_TIMEOUT    8  /* a staged page copy did not arrive within the wait limit */
 #define WUSHKV_DEV_BAD_COUNT      16  /* max_new == 1 was promised but a sequence brought more than one token: sequence skipped;
@@ -74,8 +74,9 @@ extern "C" {
 #define WUSHKV_DEV_ROPE_RANGE     64  /* a position beyond the rotary table of a *_projected call: rotated by the table's last angle */
 #define WUSHKV_DEV_POOL_EMPTY    128  /* wushkv_pages_reserve: too few free pages, none was handed out */
 #define WUSHKV_DEV_BAD_REFS      256  /* a page's reference count contradicts the page table */
-/* After PAGE_TABLE_FULL, BAD_PAGE_ID, BAD_SLOT or BAD_COUNT in wushkv_append the length of the affected
- * sequence is left as it was (tokens of the call that did fit are orphaned: nothing reads them). */
+/* wushkv_append stores a sequence's new tokens all or none.  After PAGE_TABLE_FULL, BAD_PAGE_ID, BAD_SLOT or BAD_COUNT the affected
+ * sequence is as it was: its length, windows and pages are not touched, whichever of its tokens had a page.  The other sequences
+ * of the call are appended. */
 
 /*
  * One layer's cache description.  Plain data; the caller fills it for every call.

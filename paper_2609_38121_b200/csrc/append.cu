@@ -206,32 +206,69 @@ __device__ __forceinline__ void store_v_codes(unsigned char* rec, int r, const i
     }
 }
 
-// Where a new token goes; false (with a status bit) if it cannot be stored.
+// Where a new token goes.
 struct TokenSlot {
     int b, slot, pos, s_final;
     unsigned char* rec;      // this head's record of the token's page
     int r;                   // row inside the page
 };
 
-__device__ __forceinline__ bool locate_token(const AppendParams& P, int token, int head, TokenSlot& ts) {
+// The sequence that brings a token; false if none does.
+struct TokenSequence { int b, slot, s0, first, n_new; };
+__device__ __forceinline__ bool find_sequence(const AppendParams& P, int token, TokenSequence& q) {
     int lo = 0, hi = P.batch;                 // largest b with cu_new[b] <= token
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (ld_in(P.cu_new + mid) <= token) lo = mid; else hi = mid;
     }
-    ts.b = lo;
-    ts.slot = ld_in(P.slot + lo);
-    const int s0 = ld_in(P.seq_len + lo);
-    const int first = ld_in(P.cu_new + lo), last = ld_in(P.cu_new + lo + 1);
-    ts.pos = s0 + (token - first);
-    ts.s_final = s0 + (last - first);
-    if (ts.slot < 0 || ts.slot >= P.c.n_slots || s0 < 0) { atomicOr(P.c.dev_status, WUSHKV_DEV_BAD_SLOT); return false; }
-    const int pidx = ts.pos / PAGE_TOKENS;
-    if (pidx >= P.c.max_pages) { atomicOr(P.c.dev_status, WUSHKV_DEV_PAGE_TABLE_FULL); return false; }
-    const int page = ld_in(P.c.page_table + static_cast<long long>(ts.slot) * P.c.max_pages + pidx);
-    if (page < 0 || page >= P.c.n_pages) { atomicOr(P.c.dev_status, WUSHKV_DEV_BAD_PAGE_ID); return false; }
+    q.b = lo;
+    q.slot = ld_in(P.slot + lo);
+    q.s0 = ld_in(P.seq_len + lo);
+    q.first = ld_in(P.cu_new + lo);
+    q.n_new = ld_in(P.cu_new + lo + 1) - q.first;
+    return token >= q.first && token - q.first < q.n_new;
+}
+
+// A sequence's new tokens are stored all or none: a sequence that keeps its length also keeps its windows, whose oldest ring rows
+// are those that its new tokens would take.  Status bits that refuse the n_new > 0 tokens behind s0 positions, 0 if all of their
+// pages are there.  LANES threads share out the table's entries: lane takes every LANES-th of them, and their results have to be joined.
+template <int LANES>
+__device__ __forceinline__ int refusal(const CacheView& c, int slot, int s0, int n_new, int lane) {
+    if (slot < 0 || slot >= c.n_slots || s0 < 0) return WUSHKV_DEV_BAD_SLOT;
+    const long long last_pos = static_cast<long long>(s0) + n_new - 1;
+    if (last_pos >= 0x7fffffff || last_pos / PAGE_TOKENS >= c.max_pages) return WUSHKV_DEV_PAGE_TABLE_FULL;
+    const int* row = c.page_table + static_cast<long long>(slot) * c.max_pages;
+    const int last = static_cast<int>(last_pos) / PAGE_TOKENS;
+    bool there = true;
+#pragma unroll (LANES == 1 ? 1 : 4)
+    for (int p = s0 / PAGE_TOKENS + lane; p <= last; p += LANES) {
+        const int page = ld_in(row + p);
+        there &= page >= 0 && page < c.n_pages;
+    }
+    return there ? 0 : WUSHKV_DEV_BAD_PAGE_ID;
+}
+
+// The place of a token whose sequence is not refused.
+__device__ __forceinline__ void place_token(const AppendParams& P, const TokenSequence& q, int token, int head, TokenSlot& ts) {
+    ts.b = q.b;
+    ts.slot = q.slot;
+    ts.pos = q.s0 + (token - q.first);
+    ts.s_final = q.s0 + q.n_new;
+    const int page = ld_in(P.c.page_table + static_cast<long long>(q.slot) * P.c.max_pages + ts.pos / PAGE_TOKENS);
     ts.rec = P.c.pages + (static_cast<long long>(page) * P.c.n_kv + head) * record_bytes(P.c.bits);
     ts.r = ts.pos % PAGE_TOKENS;
+}
+
+// Where a warp's token goes; false (with a status bit) if it cannot be stored.
+__device__ __forceinline__ bool locate_token(const AppendParams& P, int token, int head, int lane, TokenSlot& ts) {
+    TokenSequence q;
+    if (!find_sequence(P, token, q)) return false;
+    const unsigned bits = __reduce_or_sync(FULL, static_cast<unsigned>(refusal<32>(P.c, q.slot, q.s0, q.n_new, lane)));
+    if (bits != 0u) {
+        if (lane == 0) atomicOr(P.c.dev_status, static_cast<int>(bits));
+        return false;
+    }
+    place_token(P, q, token, head, ts);
     return true;
 }
 
@@ -272,7 +309,7 @@ __global__ void __launch_bounds__(256) append_rows_kernel(AppendParams P) {
     const int tok1 = min(tok0 + P.tokens_per_cta, P.total_new);
     for (int token = tok0 + warp; token < tok1; token += nwarps) {
         TokenSlot ts;
-        if (!locate_token(P, token, head, ts)) continue;
+        if (!locate_token(P, token, head, lane, ts)) continue;
         const long long row = (static_cast<long long>(token) * P.c.n_kv + head) * D;
         // ---------------- keys: k' = T k (Algorithm 2 line 3), fp32 accumulation of exact bf16 products
         const uint2 kraw = ld_in(reinterpret_cast<const uint2*>(P.K_new + row) + lane);
@@ -483,6 +520,12 @@ struct RowInfo {                 // where one token of the tile goes (filled onc
     int r, pos, s_final, slot;
     int pad[2];
 };
+// The place of a token of the tile as the warp-per-vector stores take it; false: skip the token.
+__device__ __forceinline__ bool row_token(const AppendParams& P, const RowInfo& ri, TokenSlot& ts) {
+    ts.b = -1; ts.slot = ri.slot; ts.pos = ri.pos; ts.s_final = ri.s_final; ts.r = ri.r;
+    ts.rec = P.c.pages + ri.rec_off;
+    return ri.rec_off >= 0;
+}
 
 __device__ __forceinline__ void ce_desc_u(unsigned& a, unsigned& b) {
     const unsigned hi = max(a, b), lo = min(a, b);
@@ -614,6 +657,7 @@ __global__ void __launch_bounds__(TC_THREADS, 2) append_chunk_kernel(AppendParam
     unsigned char* sV = tc_smem + TC_SMEM_B + TC_SMEM_A;             // value rows of the tile, until the fp32 tile arrives
     unsigned long long* mbar = reinterpret_cast<unsigned long long*>(tc_smem + TC_SMEM_B + TC_SMEM_X);
     unsigned* tmem_slot = reinterpret_cast<unsigned*>(tc_smem + TC_SMEM_B + TC_SMEM_X + 16);
+    int2* checked = reinterpret_cast<int2*>(tc_smem + TC_SMEM_B + TC_SMEM_X + 24);      // of a locating warp: the last sequence whose pages it looked at, and what refuses it
     RowInfo* rows = reinterpret_cast<RowInfo*>(tc_smem + TC_SMEM_B + TC_SMEM_X + 64);
     const int head = blockIdx.y;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -633,6 +677,7 @@ __global__ void __launch_bounds__(TC_THREADS, 2) append_chunk_kernel(AppendParam
         asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(tbar) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (tid < TC_TILE / 32) checked[tid] = make_int2(-1, 0);
     unsigned inexact = 0;
     {
         const float* T = P.c.T_K + static_cast<long long>(head) * D * D;
@@ -721,9 +766,34 @@ __global__ void __launch_bounds__(TC_THREADS, 2) append_chunk_kernel(AppendParam
         if (tid < TC_TILE) {                                  // where each token of the tile goes
             RowInfo ri;
             ri.rec_off = -1; ri.r = 0; ri.pos = 0; ri.s_final = 0; ri.slot = 0; ri.pad[0] = ri.pad[1] = 0;
-            TokenSlot ts;
-            if (tok0 + tid < P.total_new && locate_token(P, tok0 + tid, head, ts)) {
+            TokenSequence q;
+            q.b = q.slot = q.s0 = q.first = q.n_new = 0;
+            const bool brought = tok0 + tid < P.total_new && find_sequence(P, tok0 + tid, q);
+            // A sequence with tokens outside this warp's holds the warp's first or last token: the warp looks at its pages together, once
+            // for all of its tiles that follow.  The others have at most 30 tokens, two pages.
+            const unsigned held = __ballot_sync(FULL, brought);
+            bool pending = brought;
+            int bits = 0;
+            for (unsigned left = held; left != 0u;) {
+                const int from = left == held ? __ffs(held) - 1 : 31 - __clz(held), b = __shfl_sync(FULL, q.b, from);
+                int2 seen = checked[warp];
+                if (seen.x != b) {
+                    const int slot = __shfl_sync(FULL, q.slot, from), s0 = __shfl_sync(FULL, q.s0, from), n_new = __shfl_sync(FULL, q.n_new, from);
+                    seen = make_int2(b, static_cast<int>(__reduce_or_sync(FULL, static_cast<unsigned>(refusal<32>(P.c, slot, s0, n_new, lane)))));
+                    __syncwarp();
+                    if (lane == 0) checked[warp] = seen;
+                    __syncwarp();
+                }
+                if (pending && q.b == b) { bits = seen.y; pending = false; }
+                left = left == held ? __ballot_sync(FULL, pending) : 0u;
+            }
+            if (pending) bits = refusal<1>(P.c, q.slot, q.s0, q.n_new, 0);
+            if (brought && bits == 0) {
+                TokenSlot ts;
+                place_token(P, q, tok0 + tid, head, ts);
                 ri.rec_off = ts.rec - P.c.pages; ri.r = ts.r; ri.pos = ts.pos; ri.s_final = ts.s_final; ri.slot = ts.slot;
+            } else if (bits != 0) {
+                atomicOr(P.c.dev_status, bits);
             }
             rows[tid] = ri;
         }
@@ -911,9 +981,8 @@ __global__ void __launch_bounds__(TC_THREADS, 2) append_chunk_kernel(AppendParam
         } else {
             for (int v = warp; v < TC_TILE; v += TC_THREADS / 32) {
                 const int token = tok0 + v;
-                if (token >= P.total_new) break;
                 TokenSlot ts;
-                if (!locate_token(P, token, head, ts)) continue;
+                if (!row_token(P, rows[v], ts)) continue;
                 const uint2 vraw = ld_in(reinterpret_cast<const uint2*>(P.V_new + (static_cast<long long>(token) * P.c.n_kv + head) * D) + lane);
                 float x[4] = {bf16_bits_to_float(vraw.x & 0xffff), bf16_bits_to_float(vraw.x >> 16),
                               bf16_bits_to_float(vraw.y & 0xffff), bf16_bits_to_float(vraw.y >> 16)};
@@ -1052,10 +1121,8 @@ __global__ void __launch_bounds__(TC_THREADS, 2) append_chunk_kernel(AppendParam
             }
         } else {
             for (int v = warp; v < TC_TILE; v += TC_THREADS / 32) {
-                const int token = tok0 + v;
-                if (token >= P.total_new) break;
                 TokenSlot ts;
-                if (!locate_token(P, token, head, ts)) continue;
+                if (!row_token(P, rows[v], ts)) continue;
                 const float4 kp = *reinterpret_cast<const float4*>(sX + v * TC_X_PITCH + 4 * lane);
                 float x[4] = {kp.x, kp.y, kp.z, kp.w};
                 int code[4];
@@ -1078,9 +1145,8 @@ __global__ void __launch_bounds__(TC_THREADS, 2) append_chunk_kernel(AppendParam
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(128u) : "memory");
 }
 
-// Advances the lengths after a rows / chunk append.  A sequence one of whose tokens could not be stored
-// (bad slot, page table too short, page id outside the pool: the append kernel flagged it and skipped
-// that token) keeps its old length.
+// Advances the lengths after a rows / chunk append.  A sequence whose tokens were not stored (bad slot, page table too short, page
+// id outside the pool: the append kernel flagged it and skipped all of its tokens) keeps its old length.
 // One warp per sequence: its lanes look at the sequence's new pages side by side (a thread per sequence, page after page, took
 // 12 us for 8 x 8192 tokens).
 __global__ void __launch_bounds__(256) advance_len_kernel(CacheView c, int batch, const int* slot, int* seq_len, const int* cu_new) {
@@ -1090,17 +1156,9 @@ __global__ void __launch_bounds__(256) advance_len_kernel(CacheView c, int batch
     if (b >= batch) return;
     const int n_new = cu_new[b + 1] - cu_new[b];
     if (n_new <= 0) return;
-    const int s0 = seq_len[b], sl = slot[b];
-    if (sl < 0 || sl >= c.n_slots || s0 < 0) return;
-    const int p0 = s0 / PAGE_TOKENS, p1 = (s0 + n_new - 1) / PAGE_TOKENS;
-    if (p1 >= c.max_pages) return;
-    bool ok = true;
-#pragma unroll 4
-    for (int p = p0 + lane; p <= p1; p += 32) {
-        const int page = c.page_table[static_cast<long long>(sl) * c.max_pages + p];
-        ok &= page >= 0 && page < c.n_pages;
-    }
-    if (__all_sync(FULL, ok) && lane == 0) seq_len[b] = s0 + n_new;
+    const int s0 = seq_len[b];
+    const bool stored = refusal<32>(c, slot[b], s0, n_new, lane) == 0;
+    if (__all_sync(FULL, stored) && lane == 0) seq_len[b] = s0 + n_new;
 }
 
 __global__ void unpack_debug_kernel(CacheView c, int slot, int head, int which, int pos0, int n,
