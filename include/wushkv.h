@@ -440,14 +440,15 @@ int wushkv_decode_attn_sparse(const wushkv_cache* cache, int32_t batch, const in
  * The caller starts with a table of -1 and counts of 0 (or with counts that match its table).
  *
  * wushkv_pages_reserve: before wushkv_append of the tokens (seq_len, cu_new as the append will get them), gives every sequence
- *   the pages that its new tokens will be written to.  Indexes without a page get a free one.  If the last page is partly filled
- *   and other entries name it too, the sequence gets a page of its own and the old one is to be copied into it: the pair is
+ *   the pages that its new tokens will be written to, so that no other entry names them.  Indexes without a page get a free one.  If
+ *   a page that is there is named by other entries too (after a fork; also behind the length of a sequence that went back without a
+ *   release), the sequence gets a page of its own for it; a partly filled last page is to be copied into that: the pair is
  *   appended to the copy list, which the caller passes to wushkv_copy_pages before the append.  Sequences are taken in order,
  *   pages within a sequence too, free pages lowest first; if all holders of a page reserve in one call, the last keeps it.
  *     copy_src, copy_dst (device, out): int32 [batch], pairs of page ids, -1 behind them; n_copies (device, out): their number.
  *   If there are fewer free pages than the call needs, none is handed out: WUSHKV_DEV_POOL_EMPTY is set, missing pages stay
- *   missing, and the entry of a partly filled page that others name is locked, so that an append of that sequence is refused
- *   (BAD_PAGE_ID, length unchanged) and cannot write into the others' page.  A later call that succeeds unlocks it.  A sequence
+ *   missing, and the entries of pages to be written that others name are locked, so that an append of that sequence is refused
+ *   (BAD_PAGE_ID, length unchanged) and cannot write into the others' pages.  A later call that succeeds unlocks them.  A sequence
  *   whose tokens pass the table's end gets nothing (PAGE_TABLE_FULL).  Slots must be distinct (not checked).
  *   workspace (device): >= wushkv_pages_workspace_bytes(pool, batch) bytes, 4-byte aligned, scratch.
  * wushkv_pages_fork: for k < n, sequence dst_slot[k] becomes a copy of sequence src_slot[k] of src_len[k] cached positions (its

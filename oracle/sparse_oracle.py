@@ -108,18 +108,16 @@ class Pool:
             for i in range(length // PAGE, (length + new - 1) // PAGE + 1):
                 e = table[slot, i]
                 page = e if e >= 0 else -2 - e
-                if e != -1 and i == length // PAGE and length % PAGE:
+                if e != -1 and refs[page] == 1:
                     table[slot, i] = page
-                    if refs[page] == 1:
-                        continue
-                elif e != -1:
                     continue
                 if not free:
                     enough = False
                     break
                 own = free.pop(0)
                 if e != -1:
-                    copies.append((page, own))
+                    if i * PAGE < length:
+                        copies.append((page, own))
                     refs[page] -= 1
                 table[slot, i] = own
                 refs[own] = 1
@@ -128,12 +126,13 @@ class Pool:
             return copies
         self.empty = True
         for slot, length, new in requests:
-            if new <= 0 or (length + new - 1) // PAGE >= table.shape[1] or length % PAGE == 0:
+            if new <= 0 or (length + new - 1) // PAGE >= table.shape[1]:
                 continue
-            e = self.table[slot, length // PAGE]
-            if e != -1:
-                page = e if e >= 0 else -2 - e
-                self.table[slot, length // PAGE] = -2 - page if self.refs[page] > 1 else page
+            for i in range(length // PAGE, (length + new - 1) // PAGE + 1):
+                e = self.table[slot, i]
+                if e != -1:
+                    page = e if e >= 0 else -2 - e
+                    self.table[slot, i] = -2 - page if self.refs[page] > 1 else page
         return []
 
     def fork(self, src, dst, length):

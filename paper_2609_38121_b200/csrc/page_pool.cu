@@ -146,12 +146,12 @@ struct ReserveParams {
     int* copy_src;
     int* copy_dst;
     int* n_copies;
-    int* need;           // [batch]: new pages of the sequence, later their first rank
+    int* need;           // [batch]: new pages of the sequence (~ of them if it also has shared pages to be written as a whole), later their first rank
     int* shared;         // [batch]: its last page if that is shared and about to be written, else -1; later 1 + the index of its copy, or 0
     int* list;           // [n_pages]: the free pages, lowest first, as many as are needed
 };
 
-// What sequence b asks for: its first and last page index to be written; false: nothing.
+// What sequence b asks for: its first and last page index to be written, whether the first is partly filled; false: nothing.
 struct Request { int slot, first, last; bool tail; };
 __device__ __forceinline__ bool request_of(const ReserveParams& P, int b, Request& r, bool report) {
     const int s0 = P.seq_len[b], n = P.cu_new[b + 1] - P.cu_new[b];
@@ -166,6 +166,44 @@ __device__ __forceinline__ bool request_of(const ReserveParams& P, int b, Reques
     return true;
 }
 
+// Calls with shared pages that are written from their first row on (by sequences that went back without a release), by one CTA: they
+// are rare, and the table is walked once per step.  Of k holders of a page that are all here the last one keeps it, the others leave
+// it: with every entry that is to be written taken off its page's count, the pages that are left to nobody are those whose holders
+// are all here, and their keeper is the last sequence that was seen.  Leaves need and shared as the first step does, with ~ taken off,
+// the counts as they were, and a whole page that is to be left as a locked entry, one that is kept as an unlocked one.
+__device__ __noinline__ void settle_shared_pages(const ReserveParams& P, int lane, int warp) {
+    const PoolView& v = P.v;
+    int* last = P.list;                                  // [n_pages]
+    for (int step = 0; step < 4; ++step) {
+        for (int b = warp; b < P.batch; b += POOL_WARPS) {
+            Request r;
+            int need = 0, shared = -1;
+            if (request_of(P, b, r, false)) {
+                int* row = v.table + static_cast<long long>(r.slot) * v.max_pages;
+                for (int i = r.first + lane; i <= r.last; i += 32) {
+                    const int e = row[i], page = entry_page(e);
+                    if (e == -1) { need += step == 2; continue; }
+                    if (page >= v.n_pages) continue;
+                    if (step == 0) last[page] = -1;
+                    else if (step == 1) { atomicSub(v.refs + page, 1); atomicMax(last + page, b); }
+                    else if (step == 3) atomicAdd(v.refs + page, 1);
+                    else {
+                        const bool keep = __ldcg(v.refs + page) <= 0 && __ldcg(last + page) == b;
+                        if (i == r.first && r.tail) shared = keep ? -1 : page;
+                        else { row[i] = keep ? page : locked_entry(page); need += !keep; }
+                    }
+                }
+            }
+            if (step == 2) {
+                need = __reduce_add_sync(0xffffffffu, need);
+                shared = __shfl_sync(0xffffffffu, shared, 0);
+                if (lane == 0) { P.need[b] = need; P.shared[b] = shared; }
+            }
+        }
+        __syncthreads();
+    }
+}
+
 __global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS) pages_reserve_kernel(ReserveParams P) {
     pdl_wait();
     pdl_launch_dependents();
@@ -176,11 +214,13 @@ __global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS
     __shared__ int tile[POOL_THREADS];
     __shared__ int free_s, copies_s;                     // free pages of this CTA's part; CTA 0: copies asked for
     __shared__ long long total_s;                        // CTA 0: pages asked for
+    __shared__ int settled_s;                            // CTA 0: whether shared pages are left that are written as a whole
 
     // 1. what every sequence needs: a warp per sequence, a lane per page index
     for (int b = rank * POOL_WARPS + warp; b < P.batch; b += POOL_CTAS * POOL_WARPS) {
         Request r;
         int missing = 0, shared = -1;
+        bool whole = false;                              // an existing page that others name too, all of whose tokens are new
         if (request_of(P, b, r, lane == 0)) {
             const int* row = v.table + static_cast<long long>(r.slot) * v.max_pages;
             for (int i = r.first + lane; i <= r.last; i += 32) {
@@ -188,16 +228,18 @@ __global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS
                 if (e == -1) {
                     ++missing;
                     if (i == r.first && r.tail) atomicOr(v.dev_status, WUSHKV_DEV_BAD_PAGE_ID);      // its tokens are lost
-                } else if (i == r.first && r.tail) {
+                } else {
                     const int page = entry_page(e);
-                    if (page >= v.n_pages) atomicOr(v.dev_status, WUSHKV_DEV_BAD_PAGE_ID);
-                    else if (v.refs[page] > 1) shared = page;
+                    const bool tail = i == r.first && r.tail;
+                    if (page >= v.n_pages) { if (tail) atomicOr(v.dev_status, WUSHKV_DEV_BAD_PAGE_ID); }
+                    else if (v.refs[page] > 1) { if (tail) shared = page; else whole = true; }
                 }
             }
             missing = __reduce_add_sync(0xffffffffu, missing);
             shared = __shfl_sync(0xffffffffu, shared, 0);
+            whole = __any_sync(0xffffffffu, whole);
         }
-        if (lane == 0) { P.need[b] = missing; P.shared[b] = shared; }
+        if (lane == 0) { P.need[b] = whole ? ~missing : missing; P.shared[b] = shared; }
     }
     int lo, hi;
     pool_part(v.n_pages, rank, lo, hi);
@@ -206,42 +248,53 @@ __global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS
     cluster.sync();
 
     // 2. CTA 0: which shared pages are copied, and the first rank of every sequence.  The sequences are taken in order: one that
-    // finds its page still shared copies it and leaves it, so of k holders of a page that are all here the last one keeps it.
+    // finds its page still shared copies it and leaves it, so of k holders of a page that are all here the last one keeps it.  Where
+    // shared pages are written as a whole, too, the same is found out for all pages together.
     if (rank == 0) {
-        long long pages = 0;
-        int copies = 0;
-        for (int base = 0; base < P.batch; base += POOL_THREADS) {
-            const int b = base + threadIdx.x;
-            int need = 0, shared = -1;
-            if (b < P.batch) { need = P.need[b]; shared = P.shared[b]; }
-            bool copy = false;
-            if (__syncthreads_or(shared >= 0)) {
-                int earlier = 0;
-                for (int t0 = 0; t0 <= base; t0 += POOL_THREADS) {
-                    __syncthreads();
-                    // the entries of earlier tiles say in `tile` only whether they name the same page, so the list must not be rewritten yet
-                    const int o = t0 + threadIdx.x;
-                    tile[threadIdx.x] = o < P.batch ? (t0 == base ? shared : P.list[o]) : -1;
-                    __syncthreads();
-                    const int n = t0 == base ? static_cast<int>(threadIdx.x) : POOL_THREADS;
-                    if (shared >= 0)
-                        for (int k = 0; k < n; ++k) earlier += tile[k] == shared;
+        long long pages;
+        int copies;
+        bool settled = false;
+        for (;; settled = true) {
+            bool whole = false;
+            pages = 0;
+            copies = 0;
+            for (int base = 0; base < P.batch; base += POOL_THREADS) {
+                const int b = base + threadIdx.x;
+                int need = 0, shared = -1;
+                if (b < P.batch) { need = P.need[b]; shared = P.shared[b]; }
+                if (need < 0) { need = ~need; whole = true; }
+                bool copy = settled && shared >= 0;
+                if (!settled && __syncthreads_or(shared >= 0)) {
+                    int earlier = 0;
+                    for (int t0 = 0; t0 <= base; t0 += POOL_THREADS) {
+                        __syncthreads();
+                        // the entries of earlier tiles say in `tile` only whether they name the same page, so the list must not be rewritten yet
+                        const int o = t0 + threadIdx.x;
+                        tile[threadIdx.x] = o < P.batch ? (t0 == base ? shared : P.list[o]) : -1;
+                        __syncthreads();
+                        const int n = t0 == base ? static_cast<int>(threadIdx.x) : POOL_THREADS;
+                        if (shared >= 0)
+                            for (int k = 0; k < n; ++k) earlier += tile[k] == shared;
+                    }
+                    copy = shared >= 0 && v.refs[shared] - earlier > 1;
                 }
-                copy = shared >= 0 && v.refs[shared] - earlier > 1;
+                if (b < P.batch) P.list[b] = shared;         // kept for the tiles to come (the list proper is written after the next barrier)
+                int total_p, total_c;
+                const int at = block_prefix(need + (copy ? 1 : 0), &total_p, scratch);
+                const int at_copy = block_prefix(copy ? 1 : 0, &total_c, scratch);
+                if (b < P.batch) { P.need[b] = static_cast<int>(pages) + at; P.shared[b] = copy ? 1 + copies + at_copy : 0; }
+                pages += total_p;
+                copies += total_c;
             }
-            if (b < P.batch) P.list[b] = shared;         // kept for the tiles to come (the list proper is written after the next barrier)
-            int total_p, total_c;
-            const int at = block_prefix(need + (copy ? 1 : 0), &total_p, scratch);
-            const int at_copy = block_prefix(copy ? 1 : 0, &total_c, scratch);
-            if (b < P.batch) { P.need[b] = static_cast<int>(pages) + at; P.shared[b] = copy ? 1 + copies + at_copy : 0; }
-            pages += total_p;
-            copies += total_c;
+            if (settled || !__syncthreads_or(whole)) break;
+            settle_shared_pages(P, lane, warp);
         }
-        if (threadIdx.x == 0) { total_s = pages; copies_s = copies; }
+        if (threadIdx.x == 0) { total_s = pages; copies_s = copies; settled_s = settled; }
     }
     cluster.sync();
     const long long wanted = *cluster.map_shared_rank(&total_s, 0);
     const int copies = *cluster.map_shared_rank(&copies_s, 0);
+    const bool settled = *cluster.map_shared_rank(&settled_s, 0) != 0;
     int free_before = 0, free_all = 0;
     for (int r = 0; r < POOL_CTAS; ++r) {
         const int f = *cluster.map_shared_rank(&free_s, r);
@@ -295,16 +348,24 @@ __global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS
                 }
             }
         }
-        if (!granted) continue;
         for (int i0 = r.first; i0 <= r.last; i0 += 32) {
             const int i = i0 + lane;
-            const bool missing = i <= r.last && row[i] == -1;
-            const unsigned m = __ballot_sync(0xffffffffu, missing);
-            if (missing) {
-                const int own = P.list[at + __popc(m & ((1u << lane) - 1u))];
+            const bool here = i <= r.last && !(r.tail && i == r.first && row[i] != -1);
+            const int e = here ? row[i] : 0, page = here && e != -1 ? entry_page(e) : v.n_pages;
+            const bool known = page < v.n_pages;
+            if (!granted) {                              // shared pages stay shared here as well
+                if (known) row[i] = v.refs[page] > 1 ? locked_entry(page) : page;
+                continue;
+            }
+            const bool leave = known && settled && e < -1, wants = leave || (here && e == -1);
+            const unsigned m = __ballot_sync(0xffffffffu, wants);
+            const int k = at + __popc(m & ((1u << lane) - 1u));
+            if (wants && k < wanted) {                   // (always, unless a slot is named twice)
+                const int own = P.list[k];
                 row[i] = own;
                 v.refs[own] = 1;
-            }
+                if (leave) atomicSub(v.refs + page, 1);
+            } else if (known && e < -1) row[i] = page;   // locked before, and its only holder now
             at += __popc(m);
         }
     }
