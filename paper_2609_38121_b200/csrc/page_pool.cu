@@ -386,7 +386,7 @@ struct CompactParams {
     int* n_live;
     int* holes;          // [n_pages]: free pages below the number of live ones, lowest first
     int* movers;         // [n_pages]: live pages from that number on, highest first
-    int* moved;          // [n_pages]: new place of a live page from that number on, -1 of a free one
+    int* moved;          // [n_pages]: place of a live page, -1 of a page that was free
     int n_list;          // capacity of the copy list
 };
 
@@ -425,7 +425,7 @@ __global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS
             if (p + e < hi) {
                 if (p + e < live) { if (!used[e]) { P.holes[p + e - below] = p + e; ++my_holes; } }
                 else if (used[e]) P.movers[live - 1 - below] = p + e;
-                else P.moved[p + e] = -1;
+                P.moved[p + e] = used[e] ? p + e : -1;      // (of a mover written again behind the barrier)
             }
             below += used[e];
         }
@@ -455,11 +455,11 @@ __global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS
 #pragma unroll 4
     for (long long i = rank * POOL_THREADS + threadIdx.x; i < entries; i += POOL_CTAS * POOL_THREADS) {
         const int e = v.table[i], page = entry_page(e);
-        if (page < live) continue;
+        if (page < 0) continue;
         if (page >= v.n_pages) { atomicOr(v.dev_status, WUSHKV_DEV_BAD_PAGE_ID); continue; }
         const int to = P.moved[page];
         if (to < 0) { atomicOr(v.dev_status, WUSHKV_DEV_BAD_REFS); v.table[i] = -1; continue; }        // an entry that the counts do not know
-        v.table[i] = e >= 0 ? to : locked_entry(to);
+        if (to != page) v.table[i] = e >= 0 ? to : locked_entry(to);
     }
 }
 
