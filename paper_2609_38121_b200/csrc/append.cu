@@ -1246,7 +1246,7 @@ static int append_impl(const wushkv_cache* cache, int32_t batch, const int32_t* 
     P.pro = Prologue{nullptr, 0, 0, nullptr, 0.f};
     P.use_tma = 0;
     if (prologue && !make_prologue(prologue, prologue->k_norm_weight, P.pro)) return WUSHKV_EINVAL;
-    if (batch <= 0 || !slot || !seq_len || !cu_new || total_new < 0 || max_new < 0 || max_new > total_new) return WUSHKV_EINVAL;
+    if (batch <= 0 || !slot || !seq_len || !cu_new || !int_arrays(slot, seq_len, cu_new) || total_new < 0 || max_new < 0 || max_new > total_new) return WUSHKV_EINVAL;
     if (total_new == 0) return WUSHKV_OK;
     if (!K_new || !V_new || !aligned(K_new, 16) || !aligned(V_new, 16)) return WUSHKV_EINVAL;
     cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -762,7 +762,7 @@ static int decode_attn_impl(const wushkv_cache* cache, int32_t batch, const int3
     P.q_early = q_early;
     const int rc = make_view(cache, P.c);
     if (rc != WUSHKV_OK) return rc;
-    if (!slot || !seq_len || !Q || !O || !workspace || !aligned(Q, 16) || !aligned(O, 16) || !aligned(workspace, 256)) return WUSHKV_EINVAL;
+    if (!slot || !seq_len || !int_arrays(slot, seq_len) || !Q || !O || !workspace || !aligned(Q, 16) || !aligned(O, 16) || !aligned(workspace, 256)) return WUSHKV_EINVAL;
     DecodePlan pl;
     if (!make_plan(P.c, batch, max_seq_len, pl)) return WUSHKV_EINVAL;
     if (batch > 65535) return WUSHKV_EINVAL;

@@ -11,6 +11,9 @@
 namespace wushkv {
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+// Arrays of 32-bit integers that kernels read or write (null pointers pass: where they are errors they are checked on their own).
+template <class... P>
+inline bool int_arrays(P... p) { return (aligned(p, 4) && ...); }
 
 // Checks the cache description and fills the device-side view.  Returns WUSHKV_OK or WUSHKV_EINVAL / ECAPACITY.
 inline int make_view(const wushkv_cache* c, CacheView& v) {

@@ -597,7 +597,8 @@ extern "C" int wushkv_pages_reserve(const wushkv_page_pool* pool, int32_t batch,
     ReserveParams P;
     const int rc = make_pool(pool, P.v);
     if (rc != WUSHKV_OK) return rc;
-    if (batch <= 0 || batch > MAX_POOL_BATCH || !slot || !seq_len || !cu_new || !copy_src || !copy_dst || !n_copies || !workspace || !aligned(workspace, 4)) return WUSHKV_EINVAL;
+    if (batch <= 0 || batch > MAX_POOL_BATCH || !slot || !seq_len || !cu_new || !copy_src || !copy_dst || !n_copies || !workspace || !int_arrays(slot, seq_len, cu_new, copy_src, copy_dst, n_copies, workspace))
+        return WUSHKV_EINVAL;
     if (workspace_bytes < pool_workspace_ints(P.v, batch) * sizeof(int)) return WUSHKV_ECAPACITY;
     P.batch = batch; P.slot = slot; P.seq_len = seq_len; P.cu_new = cu_new;
     P.copy_src = copy_src; P.copy_dst = copy_dst; P.n_copies = n_copies;
@@ -611,7 +612,7 @@ extern "C" int wushkv_pages_fork(const wushkv_page_pool* pool, int32_t n, const 
     PoolView v;
     const int rc = make_pool(pool, v);
     if (rc != WUSHKV_OK) return rc;
-    if (n < 0 || !src_slot || !dst_slot || !src_len) return WUSHKV_EINVAL;
+    if (n < 0 || !src_slot || !dst_slot || !src_len || !int_arrays(src_slot, dst_slot, src_len)) return WUSHKV_EINVAL;
     if (n == 0) return WUSHKV_OK;
     return launched(launch_pdl(pages_fork_kernel, dim3(n), dim3(256), 0, static_cast<cudaStream_t>(stream), v, src_slot, dst_slot, src_len));
 }
@@ -620,7 +621,7 @@ extern "C" int wushkv_pages_release(const wushkv_page_pool* pool, int32_t n, con
     PoolView v;
     const int rc = make_pool(pool, v);
     if (rc != WUSHKV_OK) return rc;
-    if (n < 0 || !slot) return WUSHKV_EINVAL;
+    if (n < 0 || !slot || !int_arrays(slot, keep_len)) return WUSHKV_EINVAL;
     if (n == 0) return WUSHKV_OK;
     return launched(launch_pdl(pages_release_kernel, dim3(n), dim3(256), 0, static_cast<cudaStream_t>(stream), v, slot, keep_len));
 }
@@ -630,7 +631,7 @@ extern "C" int wushkv_pages_compact(const wushkv_page_pool* pool, int32_t* copy_
     CompactParams P;
     const int rc = make_pool(pool, P.v);
     if (rc != WUSHKV_OK) return rc;
-    if (!copy_src || !copy_dst || !n_copies || !n_live || !workspace || !aligned(workspace, 4)) return WUSHKV_EINVAL;
+    if (!copy_src || !copy_dst || !n_copies || !n_live || !workspace || !int_arrays(copy_src, copy_dst, n_copies, n_live, workspace)) return WUSHKV_EINVAL;
     if (workspace_bytes < 3 * static_cast<size_t>(P.v.n_pages) * sizeof(int)) return WUSHKV_ECAPACITY;
     P.copy_src = copy_src; P.copy_dst = copy_dst; P.n_copies = n_copies; P.n_live = n_live;
     P.holes = static_cast<int*>(workspace);
@@ -645,7 +646,7 @@ extern "C" int wushkv_copy_pages(const wushkv_cache* cache, int32_t max_copies, 
     CacheView c;
     const int rc = make_view(cache, c);
     if (rc != WUSHKV_OK) return rc;
-    if (max_copies < 0 || !copy_src || !copy_dst || !n_copies || (bounds == nullptr) != (exponents == nullptr) || !aligned(bounds, 16)) return WUSHKV_EINVAL;
+    if (max_copies < 0 || !copy_src || !copy_dst || !n_copies || !int_arrays(copy_src, copy_dst, n_copies) || (bounds == nullptr) != (exponents == nullptr) || !aligned(bounds, 16)) return WUSHKV_EINVAL;
     if (max_copies == 0) return WUSHKV_OK;
     CopyPagesParams P;
     P.pages = c.pages; P.bounds = bounds; P.exponents = exponents; P.dev_status = c.dev_status;
@@ -661,7 +662,7 @@ extern "C" int wushkv_copy_windows(const wushkv_cache* cache, int32_t n, const i
     CacheView c;
     const int rc = make_view(cache, c);
     if (rc != WUSHKV_OK) return rc;
-    if (n < 0 || n > 65535 || !src_slot || !dst_slot || !src_len) return WUSHKV_EINVAL;
+    if (n < 0 || n > 65535 || !src_slot || !dst_slot || !src_len || !int_arrays(src_slot, dst_slot, src_len)) return WUSHKV_EINVAL;
     if (n == 0) return WUSHKV_OK;
     CopyWindowsParams P;
     P.sink = c.sink_kv; P.ring = c.ring_kv; P.dev_status = c.dev_status;

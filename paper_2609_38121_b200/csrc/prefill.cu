@@ -2604,7 +2604,7 @@ static int prefill_attn_impl(const wushkv_cache* cache, int32_t batch, const int
         if (!make_prologue(prologue, prologue->k_norm_weight, P.pro) || (reinterpret_cast<uintptr_t>(prologue->q_norm_weight) & 15)) return WUSHKV_EINVAL;
         P.q_weight = prologue->q_norm_weight;
     }
-    if (batch <= 0 || !slot || !seq_len || !cu_new || total_new < 0 || max_new < 0 || max_new > total_new) return WUSHKV_EINVAL;
+    if (batch <= 0 || !slot || !seq_len || !cu_new || !int_arrays(slot, seq_len, cu_new) || total_new < 0 || max_new < 0 || max_new > total_new) return WUSHKV_EINVAL;
     if (total_new == 0) return WUSHKV_OK;
     if (!K_new || !V_new || !Q_new || !O || !workspace || !aligned(K_new, 16) || !aligned(V_new, 16) || !aligned(Q_new, 16) ||
         !aligned(O, 16) || !aligned(workspace, 256))

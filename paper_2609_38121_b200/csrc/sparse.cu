@@ -188,7 +188,7 @@ static int sparse_impl(const wushkv_cache* cache, int32_t batch, const int32_t* 
     const int rc = make_view(cache, P.c);
     if (rc != WUSHKV_OK) return rc;
     if (batch <= 0 || batch > 65535 || P.c.n_kv > 65535 || max_seq_len <= 0 || n_select <= 0 || n_select > MAX_LIST) return WUSHKV_EINVAL;
-    if (!slot || !seq_len || !Q || !selected || !aligned(Q, 16) || !aligned(bounds, 16) || !aligned(O, 16)) return WUSHKV_EINVAL;
+    if (!slot || !seq_len || !Q || !selected || !int_arrays(slot, seq_len, selected) || !aligned(Q, 16) || !aligned(bounds, 16) || !aligned(O, 16)) return WUSHKV_EINVAL;
     P.pro = Prologue{nullptr, 0, 0, nullptr, 0.f};
     if (prologue && !make_prologue(prologue, prologue->q_norm_weight, P.pro)) return WUSHKV_EINVAL;
     const long long candidates = std::max<long long>(candidate_bound(P.c, max_seq_len), 1);
@@ -213,7 +213,7 @@ extern "C" int wushkv_update_page_bounds(const wushkv_cache* cache, int32_t batc
     BoundsParams P;
     const int rc = make_view(cache, P.c);
     if (rc != WUSHKV_OK) return rc;
-    if (batch <= 0 || batch > 65535 || max_new < 0 || !slot || !seq_len || !cu_new || !bounds || !exponents || !aligned(bounds, 16)) return WUSHKV_EINVAL;
+    if (batch <= 0 || batch > 65535 || max_new < 0 || !slot || !seq_len || !cu_new || !int_arrays(slot, seq_len, cu_new) || !bounds || !exponents || !aligned(bounds, 16)) return WUSHKV_EINVAL;
     if (max_new == 0) return WUSHKV_OK;
     P.slot = slot; P.seq_len = seq_len; P.cu_new = cu_new; P.bounds = bounds; P.exponents = exponents;
     const long long pages = (static_cast<long long>(max_new) + PAGE_TOKENS - 2) / PAGE_TOKENS + 1;       // that max_new consecutive tokens can touch
