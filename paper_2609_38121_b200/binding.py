@@ -476,6 +476,8 @@ class PagedCache:
         self.max_pages = (max_seq_len + page_tokens - 1) // page_tokens
         if pool is not None and (pool.n_slots, pool.max_pages) != (n_slots, self.max_pages):
             raise ValueError("the pool's page table has other slots or lengths than this cache")
+        if pool is not None and page_order is not None:
+            raise ValueError("page_order lays out pages that a pool hands out")
         n_pages = n_slots * self.max_pages if pool is None else pool.n_pages
         self.page_bytes = page_bytes(n_kv, d, bits, page_tokens)
         self.pages = torch.zeros(n_pages * self.page_bytes, dtype=torch.uint8, device=self.device)
