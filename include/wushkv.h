@@ -398,9 +398,9 @@ int wushkv_decode_step_host(const wushkv_cache* cache, int32_t batch, const int3
  * after the conversion of the sum and after the product.  A page's key is max over the query heads of the group of
  * (s - largest s of all pages of that head): how far the page is, for the head it matters most to, below that head's best page.
  * The n_select pages with the largest keys are taken, of equal keys the lower index.  The result depends on the inputs alone.
- * A query that is zero or not finite scores 0 everywhere.  Sequences may have up to 1 048 576 cached positions
- * (WUSHKV_ECAPACITY for a larger max_seq_len); one that exceeds max_seq_len is flagged with BAD_COUNT and its pages beyond are not
- * candidates.
+ * A query that is zero or not finite scores 0 everywhere.  Up to 16384 packed pages of a sequence can be ranked, those of every
+ * max_seq_len up to 1 048 576 and, as the windows take positions out, of some that are larger: WUSHKV_ECAPACITY if a sequence of
+ * max_seq_len positions has more.  One that exceeds max_seq_len is flagged with BAD_COUNT and its pages beyond are not candidates.
  *
  * Attention.  wushkv_decode_attn_selected attends to the windows and the listed pages:
  *   selected (device): int32 [batch][n_kv][n_select]; of a row the first min(n_select, packed pages) entries are read; they must
