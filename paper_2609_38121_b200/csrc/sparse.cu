@@ -216,8 +216,11 @@ extern "C" int wushkv_update_page_bounds(const wushkv_cache* cache, int32_t batc
     if (batch <= 0 || batch > 65535 || max_new < 0 || !slot || !seq_len || !cu_new || !int_arrays(slot, seq_len, cu_new) || !bounds || !exponents || !aligned(bounds, 16)) return WUSHKV_EINVAL;
     if (max_new == 0) return WUSHKV_OK;
     P.slot = slot; P.seq_len = seq_len; P.cu_new = cu_new; P.bounds = bounds; P.exponents = exponents;
-    const long long pages = (static_cast<long long>(max_new) + PAGE_TOKENS - 2) / PAGE_TOKENS + 1;       // that max_new consecutive tokens can touch
-    const dim3 grid(static_cast<unsigned>((pages * P.c.n_kv + BOUNDS_WARPS - 1) / BOUNDS_WARPS), batch);
+    // pages that max_new consecutive tokens can touch, and of those behind the table's end one, for the flag
+    const long long pages = std::min<long long>((static_cast<long long>(max_new) + PAGE_TOKENS - 2) / PAGE_TOKENS, P.c.max_pages) + 1;
+    const long long units = pages * P.c.n_kv;
+    if (units > 0x7fffffff - BOUNDS_WARPS) return WUSHKV_ECAPACITY;
+    const dim3 grid(static_cast<unsigned>((units + BOUNDS_WARPS - 1) / BOUNDS_WARPS), batch);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return launch_pdl(P.c.bits == 2 ? page_bounds_kernel<2> : P.c.bits == 3 ? page_bounds_kernel<3> : page_bounds_kernel<4>, grid, dim3(BOUNDS_WARPS * 32), 0, st, P) == cudaSuccess
         ? WUSHKV_OK : WUSHKV_ECUDA;

@@ -3,7 +3,7 @@ import pytest
 
 from oracle import sparse_oracle as S
 from paper_2609_38121_b200 import binding as B
-from tests.test_abi_sparse import SELECT, SPARSE, _cache
+from tests.test_abi_sparse import BOUNDS, SELECT, SPARSE, _cache
 
 WINDOWS = [(4, 64, 1, 0), (0, 1, 1, 0), (130, 64, 8, 0), (4, 128, 1, 3), (4, 32, 16, 0)]
 
@@ -24,3 +24,8 @@ def test_the_first_length_beyond_is_refused(s_sink, s_keep, s_flush, lag):
     for fn, args in ((B.lib.wushkv_select_pages, SELECT), (B.lib.wushkv_decode_attn_sparse, SPARSE)):
         for length in (n + 1, n + 64, (1 << 31) - 1):
             assert fn(*{**args, "cache": cache, "max_seq_len": length}.values(), None) == B.ECAPACITY, length
+
+
+def test_more_bounds_than_a_grid_holds_are_refused():
+    huge = _cache(n_q=65535, n_kv=65535, max_pages=1 << 20)
+    assert B.lib.wushkv_update_page_bounds(*{**BOUNDS, "cache": huge, "max_new": 1 << 30}.values(), None) == B.ECAPACITY
