@@ -204,7 +204,7 @@ __device__ __noinline__ void settle_shared_pages(const ReserveParams& P, int lan
     }
 }
 
-__global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS) pages_reserve_kernel(ReserveParams P) {
+__global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS) pages_reserve_kernel(const __grid_constant__ ReserveParams P) {
     pdl_wait();
     pdl_launch_dependents();
     cg::cluster_group cluster = cg::this_cluster();
@@ -350,8 +350,9 @@ __global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS
         }
         for (int i0 = r.first; i0 <= r.last; i0 += 32) {
             const int i = i0 + lane;
-            const bool here = i <= r.last && !(r.tail && i == r.first && row[i] != -1);
-            const int e = here ? row[i] : 0, page = here && e != -1 ? entry_page(e) : v.n_pages;
+            const int e = i <= r.last ? row[i] : 0;
+            const bool here = i <= r.last && !(r.tail && i == r.first && e != -1);
+            const int page = here && e != -1 ? entry_page(e) : v.n_pages;
             const bool known = page < v.n_pages;
             if (!granted) {                              // shared pages stay shared here as well
                 if (known) row[i] = v.refs[page] > 1 ? locked_entry(page) : page;
