@@ -241,7 +241,7 @@ int wushkv_decode_attn(const wushkv_cache* cache, int32_t batch, const int32_t* 
  * the quantized middle from the packed pages.  boundary_lag = n_new reproduces Algorithm 2 literally (boundary
  * moved after attention); ring_cap must then cover s_keep + s_flush - 1 + boundary_lag positions.
  *   slot, cu_new, total_new, max_new, K_new, V_new: exactly what the preceding wushkv_append received.
- *   seq_len (device): int32 [batch], the lengths AFTER that append.
+ *   seq_len (device): int32 [batch], the lengths AFTER that append.  (Rows of O of a sequence that the append refused mean nothing.)
  *   Q_new (device): bf16 [total_new][n_q][d] post-Norm post-RoPE queries of the chunk, NOT compensated.
  *   O (device, out): fp32 [total_new][n_q][d] in the folded value basis.
  *   workspace (device): >= wushkv_prefill_workspace_bytes() bytes, 256-byte aligned, scratch.
@@ -384,6 +384,8 @@ int wushkv_decode_step_host(const wushkv_cache* cache, int32_t batch, const int3
  *   exponents (device): int8 [n_pages][n_kv].
  * Over the tokens of the page that exist, with khat = x_min + Delta code rounded to fp32:
  *   e = least integer >= -31 with max |khat| <= 127 * 2^e,  lower = floor(min khat / 2^e),  upper = ceil(max khat / 2^e).
+ * Tokens that a window holds as well count like the others.  So the first page's bounds hold the sink's keys: for a head whose sink has by
+ * far its largest logit that page is listed ahead of the others, and the others' keys (below) are distances from the sink's score.
  * wushkv_update_page_bounds computes them for all pages that hold one of the positions [seq_len[b] - n_new[b], seq_len[b]),
  * n_new[b] = cu_new[b+1] - cu_new[b]: call it after wushkv_append with the same slot, cu_new and max_new (a larger max_new is
  * fine, a smaller one leaves pages out), seq_len being the lengths after that append.  The pages of other positions are left as
@@ -406,7 +408,9 @@ int wushkv_decode_step_host(const wushkv_cache* cache, int32_t batch, const int3
  *   selected (device): int32 [batch][n_kv][n_select]; of a row the first min(n_select, packed pages) entries are read; they must
  *   be distinct; -1 is skipped, an index outside the sequence's packed pages is skipped and flagged with BAD_PAGE_ID.  Positions
  *   of a listed page that a window holds are read from the window, as always.  Lists need not come from wushkv_select_pages.
- *   O (device, out): bf16 [batch][n_q][d], 16-byte aligned (the rounding is smaller than what a selection leaves out).
+ *   O (device, out): bf16 [batch][n_q][d], 16-byte aligned.  (The rounding is smaller than what a selection leaves out.  Where a list
+ *   holds all packed pages, as for sequences that have no more than n_select, this is dense attention rounded to bf16;
+ *   wushkv_decode_attn gives it in fp32.)
  * wushkv_decode_attn_sparse is both in one launch.  selected may be NULL there: the list is then kept in workspace (device,
  * 256-byte aligned, >= wushkv_sparse_workspace_bytes() bytes, scratch), which is not used otherwise and may then be NULL.
  * prologue: NULL, or the Norm / RoPE of projected queries (as in wushkv_decode_attn_projected).

@@ -426,6 +426,9 @@ __device__ __forceinline__ void page_scores(unsigned rec_k, unsigned rec_meta, c
 }
 
 // The page's probabilities and its values' contribution (value codes at shared-memory address rec_v); fmul: the heads' multipliers.
+// Probability times value step is rounded to one fp16 (half a step: 2^-11 of it, an eighth of what an output in bf16 loses, and the
+// tokens' errors average out), so that one MMA serves a block; the sums l and z and the accumulators stay in 32 bits.  Window
+// probabilities, whose values are not quantized, are taken as two bf16 terms.
 template <int BITS, int MODE>
 __device__ __forceinline__ void page_values(WarpState<MODE>& st, unsigned rec_v, const float (&sc)[4][2 * WarpState<MODE>::NH], const unsigned (&vmeta)[4][2],
                                             const float (&fmul)[WarpState<MODE>::NH], int lane) {

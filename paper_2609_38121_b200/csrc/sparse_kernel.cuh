@@ -358,8 +358,9 @@ __global__ void __launch_bounds__(NT, 512 / NT) sparse_decode_kernel(SparseParam
     if (tid == 0) sh.n_list = 0;
     // ---- q': this thread's rows of T_K^{-T} and its share of the queries are requested ahead of everything else
     // Rows per thread: a query element read from shared memory serves all of them.  Four with CTAs of four warps, whose SMs are busy with
-    // other pairs meanwhile (64 ragged sequences x 8 heads: 43.8 -> 42.2 us); two where the chain of one CTA counts (with four rows 1 x 2k
-    // tokens take the same 9.9 us, 16 x 32k 26.9 instead of 26.75 us, the selection alone 9.6 instead of 9.3 us).
+    // other pairs meanwhile (64 ragged sequences x 8 heads, 4 bits, graphs of one state: 39.6 -> 37.4 us); two where the chain of one CTA
+    // counts, to which four make no difference beyond 1 % either way (1 x 2k tokens 9.3 and 9.3 us, 16 x 32k 24.3 and 24.0, its selection
+    // alone 9.4 and 9.5).
     constexpr int ROWS = D / CL, RPT = NT == 128 ? 4 : 2;
     constexpr int SPACING = ROWS / RPT, TPR = NT / SPACING, QUADS = D / 4 / TPR;              // rows apart, threads per row, float4 per thread and row
     constexpr int PART = QUADS * RPT > 8 ? 8 / RPT : QUADS;                                  // of them in flight together
@@ -874,15 +875,16 @@ static int launch_sparse_cl(SparseParams P, cudaStream_t st) {
 template <int BITS, int MODE>
 static int launch_sparse_mode(const SparseParams& P, cudaStream_t st) {
     // CTAs per (sequence, KV head): more than one only while they all find an SM and each warp still has more than a tile of pages to
-    // score or more than two pages to attend to.  (16 x 8 heads of 510 pages, 64 selected: one CTA 27.0 us, two 28.5, one of 16 warps
-    // 26.0: a cluster's barriers and remote loads cost more than half of the scoring saves.  1 x 8 heads of 2045 pages, 128 selected:
-    // 1, 2, 4, 8 CTAs take 50.7, 36.6, 26.2, 20.7 us.)
+    // score or more than two pages to attend to.  (Graphs of one state: 16 x 8 heads of 510 pages, 64 selected: one CTA 24.1 us, two 26.7,
+    // four 39.3: a cluster's barriers and remote loads cost more than half of the scoring saves.  1 x 8 heads of 2045 pages, 128 selected:
+    // 1, 2, 4, 8 CTAs take 51.2, 36.5, 25.8, 20.3 us.)
     const long long pairs = static_cast<long long>(P.batch) * P.c.n_kv;
     const long long work = std::max<long long>(P.bounds ? P.max_candidates / 16 : 0, P.O ? P.n_select / 2 : 0);
     int offset, cl = knobs().select_cluster;
     // More pairs than CTAs of 8 warps are resident: CTAs of 4 warps, so that pairs in different steps overlap (64 ragged sequences x 8
-    // heads, 4 bits: 50.3 -> 42.2 us; 352 to 1024 pairs of 4 query heads 2 to 8 % faster, one case 1 % slower; 128 to 288 pairs 8 to 30 %
-    // slower).  With more than 4 query heads the fixed part of a pair is too long for 4 warps (512 pairs: 51.0 against 60.3 us).
+    // heads, 4 bits, graphs of one state: 48.8 -> 39.6 us, 37.4 with the four rows per thread that they take; 16 x 8 heads, for which they are
+    // not taken, 24.1 -> 30.6; when they came, 352 to 1024 pairs of 4 query heads ran 2 to 8 % faster, one case 1 % slower, 128 to 288 pairs 8 to
+    // 30 % slower).  With more than 4 query heads the fixed part of a pair is too long for 4 warps (512 pairs: 51.0 us with 8, 60.3 with 4).
     if constexpr (MODE == 0) {
         const bool small = cl == 0 ? pairs > 2 * sm_count() : cl == -1;
         if (small && sparse_smem<BITS, MODE, 128>(P, 1, offset) <= SPARSE_SMEM_MAX / 2) return launch_sparse_cl<BITS, MODE, 1, 128>(P, st);
