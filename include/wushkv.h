@@ -453,7 +453,8 @@ int wushkv_decode_attn_sparse(const wushkv_cache* cache, int32_t batch, const in
  *   If there are fewer free pages than the call needs, none is handed out: WUSHKV_DEV_POOL_EMPTY is set, missing pages stay
  *   missing, and the entries of pages to be written that others name are locked, so that an append of that sequence is refused
  *   (BAD_PAGE_ID, length unchanged) and cannot write into the others' pages.  A later call that succeeds unlocks them.  A sequence
- *   whose tokens pass the table's end gets nothing (PAGE_TABLE_FULL).  Slots must be distinct (not checked).
+ *   whose tokens pass the table's end gets nothing (PAGE_TABLE_FULL); the entry of a partly filled last page that others name is locked
+ *   for it as well.  Slots must be distinct (not checked).
  *   workspace (device): >= wushkv_pages_workspace_bytes(pool, batch) bytes, 4-byte aligned, scratch.
  * wushkv_pages_fork: for k < n, sequence dst_slot[k] becomes a copy of sequence src_slot[k] of src_len[k] cached positions (its
  *   current length): their pages are shared.  What dst_slot[k] held before is given back.  A destination must not be another

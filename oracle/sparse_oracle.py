@@ -101,6 +101,12 @@ class Pool:
 
     def reserve(self, requests):
         """requests: (slot, length, new tokens).  Returns the copies as (source, destination) pairs."""
+        for slot, length, new in requests:                         # tokens behind the table's end: nothing, a shared last page is locked
+            if new > 0 and (length + new - 1) // PAGE >= self.table.shape[1] and length % PAGE and length // PAGE < self.table.shape[1]:
+                e = self.table[slot, length // PAGE]
+                page = e if e >= 0 else -2 - e
+                if e != -1 and self.refs[page] > 1:
+                    self.table[slot, length // PAGE] = -2 - page
         table, refs, free, copies, enough = self.table.copy(), self.refs.copy(), self._free(), [], True
         for slot, length, new in requests:
             if new <= 0 or (length + new - 1) // PAGE >= table.shape[1]:

@@ -153,16 +153,22 @@ struct ReserveParams {
 };
 
 // What sequence b asks for: its first and last page index to be written, whether the first is partly filled; false: nothing.
-struct Request { int slot, first, last; bool tail; };
+// beyond: nothing, because its tokens pass the table's end (slot, first and tail are set).
+struct Request { int slot, first, last; bool tail, beyond; };
 __device__ __forceinline__ bool request_of(const ReserveParams& P, int b, Request& r, bool report) {
     const int s0 = P.seq_len[b], n = P.cu_new[b + 1] - P.cu_new[b];
     r.slot = P.slot[b];
+    r.beyond = false;
     if (r.slot < 0 || r.slot >= P.v.n_slots) { if (report) atomicOr(P.v.dev_status, WUSHKV_DEV_BAD_SLOT); return false; }
     if (n <= 0 || s0 < 0) return false;
     r.first = s0 / PAGE_TOKENS;
     r.tail = s0 % PAGE_TOKENS != 0;
     const long long last = (static_cast<long long>(s0) + n - 1) / PAGE_TOKENS;
-    if (last >= P.v.max_pages) { if (report) atomicOr(P.v.dev_status, WUSHKV_DEV_PAGE_TABLE_FULL); return false; }
+    if (last >= P.v.max_pages) {
+        if (report) atomicOr(P.v.dev_status, WUSHKV_DEV_PAGE_TABLE_FULL);
+        r.beyond = true;
+        return false;
+    }
     r.last = static_cast<int>(last);
     return true;
 }
@@ -240,6 +246,12 @@ __global__ void __cluster_dims__(POOL_CTAS, 1, 1) __launch_bounds__(POOL_THREADS
             missing = __reduce_add_sync(0xffffffffu, missing);
             shared = __shfl_sync(0xffffffffu, shared, 0);
             whole = __any_sync(0xffffffffu, whole);
+        } else if (r.beyond && r.tail && r.first < v.max_pages && lane == 0) {
+            // The append refuses the sequence, and what follows an append (the page's bounds up to this sequence's length) must not
+            // reach a page that others read further: locked, as where the pool is empty.
+            int* entry = v.table + static_cast<long long>(r.slot) * v.max_pages + r.first;
+            const int page = entry_page(*entry);
+            if (page >= 0 && page < v.n_pages && v.refs[page] > 1) *entry = locked_entry(page);
         }
         if (lane == 0) { P.need[b] = whole ? ~missing : missing; P.shared[b] = shared; }
     }
