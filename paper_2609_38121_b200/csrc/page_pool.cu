@@ -9,7 +9,7 @@
 // reserve and compact need ranks over the whole pool (the k-th free page).  They run as ONE cluster of eight CTAs: every CTA
 // counts its eighth of the pool, the counts meet at a cluster barrier, and a second walk writes each page's rank, so that a
 // call is one launch.  What bounds them is latency (the barriers and the dependent loads table entry -> count), not the 4 bytes
-// per page and entry that they read: 7.0 to 7.5 us to compact 4700 live pages of 64 sequences into the room of 32 that ended, 9.0 us to
+// per page and entry that they read: 7.2 us to compact 4700 live pages of 64 sequences into the room of 32 that ended, 8.6 us to
 // reserve for 12 forked sequences.  (The first form took 7.9 and 8.1 us; one CTA of 1024 threads without cluster barriers 14.0 and
 // 9.8 in its place.)
 //
@@ -178,7 +178,7 @@ __device__ __forceinline__ bool request_of(const ReserveParams& P, int b, Reques
 // it: with every entry that is to be written taken off its page's count, the pages that are left to nobody are those whose holders
 // are all here, and their keeper is the last sequence that was seen.  Leaves need and shared as the first step does, with ~ taken off,
 // the counts as they were, and a whole page that is to be left as a locked entry, one that is kept as an unlocked one.  (12 sequences
-// that write a whole shared page each: 12.8 us for the call, with partly filled ones 9.0.)
+// that write a whole shared page each: 12.3 us for the call, with partly filled ones 8.6.)
 __device__ __noinline__ void settle_shared_pages(const ReserveParams& P, int lane, int warp) {
     const PoolView& v = P.v;
     int* last = P.list;                                  // [n_pages]
