@@ -463,7 +463,8 @@ int wushkv_decode_attn_sparse(const wushkv_cache* cache, int32_t batch, const in
  *   that goes on from a shorter length needs its recent window in the ring: the ring holds the last ring_cap positions written.
  *   The same slot may be named twice.
  * wushkv_pages_compact: moves the live pages to the ids 0 .. live - 1: the k-th live page with an id >= live (ascending) goes to
- *   the k-th free id below.  Table and counts are rewritten, locked entries stay locked.
+ *   the k-th free id below.  Table and counts are rewritten, locked entries stay locked, an entry that
+ *   names a free page is cleared and flagged (BAD_REFS).
  *     copy_src, copy_dst (device, out): int32 [(n_pages + 1) / 2], pairs for wushkv_copy_pages, -1 behind them;
  *     n_copies, n_live (device, out): int32 each.  workspace as above (any batch).
  *   The copies must be done (every layer) before the next call that reads or writes pages.
